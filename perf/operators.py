@@ -241,7 +241,7 @@ def prepare(case, seed):
         T, B = s["T"], case["B"]
         s["outs"] = {"cu_q": torch.empty(B + 1, dtype=torch.int32, device="cuda"), "kv_len_out": torch.empty_like(s["kv_len"]),
                      "positions": torch.empty(T, dtype=torch.int32, device="cuda"), "slots": torch.empty(T, dtype=torch.int64, device="cuda"),
-                     "taken_out": torch.empty(2, dtype=torch.int32, device="cuda")}
+                     "taken_out": torch.empty(1, dtype=torch.int32, device="cuda")}
     elif case["kind"] == "append":
         s.update(_append_inputs(case, seed))
         s["out"] = torch.empty((case["T"], case["Hq"] * case["D"]), dtype=torch.float16, device="cuda")
@@ -275,9 +275,8 @@ def _plain_slots(s):
     page = torch.where(at < W * ps, table[b, (at // ps).clamp(0, W - 1)], -1).long()
     slots = torch.where(real & (page >= 0), page * ps + at % ps, -1)
     positions = torch.where(real, at, 0).to(torch.int32)
-    taken = torch.stack([(s["taken"][0] + need.sum()).clamp(max=free.numel()), (real & (slots < 0)).sum()])
     return {"table": table, "cu_q": cu.to(torch.int32), "kv_len_out": end.to(torch.int32), "positions": positions, "slots": slots,
-            "taken_out": taken.to(torch.int32)}
+            "taken_out": (s["taken"] + need.sum()).to(torch.int32)}
 
 
 def _hadamard(D, dtype):
@@ -424,7 +423,7 @@ def _exact_slots(case, seed):
     ps, W, T = case["ps"], case["W"], d["T"]
     kv, q = _slot_lengths(case)
     table, free = d["table"].cpu().tolist(), d["free"].cpu().tolist()
-    taken, missing, cu, positions, slots = 0, 0, [0], [], []
+    taken, cu, positions, slots = 0, [0], [], []
     for b, (n, m) in enumerate(zip(kv, q)):
         for col in range(-(-n // ps), min(W, -(-(n + m) // ps))):
             table[b][col] = free[taken] if taken < len(free) else -1
@@ -433,12 +432,11 @@ def _exact_slots(case, seed):
             page = table[b][p // ps] if p // ps < W else -1
             positions.append(p)
             slots.append(page * ps + p % ps if page >= 0 else -1)
-            missing += page < 0
         cu.append(cu[-1] + m)
     pad = T - cu[-1]
     return {"table": _int32(table), "cu_q": _int32(cu), "kv_len_out": _int32([a + b for a, b in zip(kv, q)]),
             "positions": _int32(positions + [0] * pad), "slots": torch.tensor(slots + [-1] * pad, dtype=torch.int64, device="cuda"),
-            "taken_out": _int32([min(taken, len(free)), missing])}
+            "taken_out": _int32([taken])}
 
 
 def _exact_append(case, seed):
