@@ -522,6 +522,97 @@ int pq_calibrate_static_zp(const void* x_cal_f16, int64_t T, int64_t K, int32_t 
                            int32_t n_gamma, int32_t n_beta, float gamma_min, float beta_min,
                            float* result, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- serving on a paged KV cache of 4-bit codes ---------------------------------------------
+ * (Table 1: the KV cache in 4 bits, static per head (O2) or dynamic per group (O1); App. B "Online Rotation": R3 on queries and
+ * keys after the position rotation; Eq. 3: attention behind prefix tokens in full precision.)  Three calls make a step of a server:
+ * pq_kv4_slots gives the new tokens of every request their places, pq_kv4_append turns the step's queries, keys and values and
+ * writes the codes to those places, pq_kv4_attention reads them.  All lengths, tables and slots lie on the device, so a
+ * captured step follows them; nothing that they hold takes a kernel outside the buffers that the arguments describe.
+ *
+ * A cache of one layer: `n_pages` pages of `page_size` tokens (a power of two in [16, 1024]) for n_kv_heads heads of head_dim (64 or
+ * 128) channels.
+ *   k_codes, v_codes  uint8 [n_pages, n_kv_heads, page_size, head_dim / 2], canonical nibbles, 16-byte aligned;
+ *   k_scale, v_scale  group = 0: static steps, fp32 [n_kv_heads], finite and positive (not checked: they live on the device);
+ *                     group = 32, 64 or 128 (at most head_dim): dynamic steps, fp32 [n_pages, n_kv_heads, page_size, head_dim / group],
+ *                     16-byte aligned, written by pq_kv4_append.
+ * The struct itself lies on the host and is read during the call. */
+typedef struct pq_kv4_cache {
+    void* k_codes;
+    void* v_codes;
+    float* k_scale;
+    float* v_scale;
+    int64_t n_pages;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page_size;
+    int32_t group;
+} pq_kv4_cache;
+
+/* Places for the new tokens of a step.  Request b has kv_len[b] tokens in the cache and q_len[b] new ones (negative counts as 0); its
+ * pages are block_table[b, 0..], a row of table_pages int32 entries.  With ps = page_size:
+ *     before_b = min(table_pages, ceil(kv_len[b] / ps)),   need_b = min(table_pages, ceil((kv_len[b] + q_len[b]) / ps)) - before_b;
+ *     the requests take free_pages[taken ...] in their order: block_table[b, before_b ..] = the next need_b of them, -1 where the
+ *         list of n_free has ended;
+ *     cu_q[b] = sum of q_len before b (B + 1 entries),   kv_len_out[b] = kv_len[b] + q_len[b];
+ *     row cu_q[b] + i:  positions = position_offset + kv_len[b] + i,   slots = page * ps + place in the page, or -1 for a token that no
+ *         page holds (list ended, table full, entry negative);
+ *     taken_out[0] = taken + sum of need_b: above n_free if the list was too short.
+ * Rows behind the last request up to T (a padded step) get position 0 and slot -1; tokens past row T are not written.  position_offset:
+ * the prefix tokens in front (>= 0).  taken: device int32, or NULL for 0; with taken_out of the last call the list is used on.
+ * All arrays int32 and 4-byte aligned but slots (int64 [T], 8-byte aligned); positions [T].  Outputs may not lie over kv_len, q_len or taken
+ * (PQ_ERR_UNSUPPORTED).  B >= 0, T >= 0 and below 2^31; table_pages >= 1; n_free >= 0.
+ */
+int pq_kv4_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t* block_table, int32_t table_pages,
+                 const int32_t* free_pages, int32_t n_free, const int32_t* taken, int32_t page_size, int64_t T, int32_t position_offset,
+                 int32_t* cu_q, int32_t* kv_len_out, int32_t* positions, int64_t* slots, int32_t* taken_out, void* stream);
+
+/* Queries, keys and values of a step, from the fused projection's output to attention's inputs, in one pass.
+ * qkv_f16   in  [T, (n_heads + 2 n_kv_heads) * head_dim] fp16: query heads, key heads, value heads; rows row_stride values apart
+ *               (a multiple of 8).
+ * Queries and keys, head by head:
+ *     y = x / sqrt(mean x^2 + eps) * w      (q_weight / k_weight: fp16 [head_dim], 16-byte aligned, or NULL: no norm; eps >= 0),
+ *     y_a, y_b = y_a cos - y_b sin, y_b cos + y_a sin     for the pairs (a, b) of the first rotary_dim channels: (i, i + rotary_dim / 2),
+ *         or (2i, 2i + 1) if interleaved != 0; cos and sin of pair i at cos_sin[position, i] and cos_sin[position, rotary_dim / 2 + i]
+ *         (cos_sin: fp32 [max_positions, rotary_dim], 16-byte aligned, or NULL: no position rotation; rotary_dim a multiple of 16, at
+ *         most head_dim; positions: int32 [T], clamped to the table),
+ *     z = head_dim-point Hadamard rotation of pq_rotate_quant if rotate != 0.
+ * q_out_f16 out [T, n_heads * head_dim] fp16: the queries' z (fp32 path, rounded once); may not lie over qkv (PQ_ERR_UNSUPPORTED).
+ * Keys' z and values' x go to slots[t] (int64: page * page_size + place) of the cache as clamp(round_half_even(z / step), -8, 7): with
+ *     group = 0 the head's static step, else step = fp32(clip * max |z| over the group / 7), 1 for a group of zeros, which is
+ *     written as well; clip in (0, 1].  The codes are those of this definition in double precision (dynamic steps: of an fp32 step within
+ *     2^-22 of it).
+ * Tokens whose slot lies outside the cache (-1 of a padded step) are neither read nor written, in the cache and in q_out.  Two tokens with the
+ * same slot leave the codes of either.  T * (n_heads + 2 n_kv_heads) < 2^31.
+ */
+int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* positions, const int64_t* slots,
+                  const void* q_weight_f16, const void* k_weight_f16, float eps, const float* cos_sin, int64_t max_positions,
+                  int32_t rotary_dim, int32_t interleaved, int32_t rotate, float clip, const pq_kv4_cache* cache, void* q_out_f16,
+                  void* stream);
+
+/* Attention over the cache, from one token of a request to whole prompts, ragged.
+ *     out[cu_q[b] + i] = softmax(softmax_scale * q . [k'; k]) [v'; v]      (Eq. 3)
+ * over the n_prefix tokens k', v' (fp16, every query sees them) and the tokens t of request b's pages with
+ *     t < kv_len[b] - (q_len - 1 - i)  if causal != 0 (the queries are the last q_len = cu_q[b + 1] - cu_q[b] cached tokens),
+ *     t < kv_len[b]                    otherwise;
+ * query head h reads key/value head h / (n_heads / n_kv_heads).  Keys and values are code * step.  A query that sees nothing gets zeros.
+ * q_f16     in  [T, n_heads * head_dim] fp16, rows row_stride values apart (a multiple of 8).
+ * cu_q      in  int32 [B + 1], ascending;  kv_len: int32 [B], the new tokens included;  block_table: int32 [B, table_pages].
+ *               kv_len is cut off at the table's pages; tokens of entries outside [0, n_pages) count as not seen.
+ * max_q     the most queries of a request: a hint that chooses between kernels, results do not depend on it (>= 1).
+ * prefix_k, prefix_v  in fp16 [n_prefix, n_kv_heads, head_dim] (rotated like the keys), NULL iff n_prefix = 0; n_prefix <= 1024.
+ * out_f16   out [T, n_heads * head_dim] fp16; rows outside [cu_q[0], cu_q[B]) are left as they were; may not lie over q.
+ * Scores, sums and the softmax's statistics are fp32; the probabilities are rounded to fp16 for the second product, and the sum that divides
+ * it is theirs.  Sums are taken in an order that depends on the sizes and lengths alone: results are reproducible.
+ * workspace: device memory, 256-byte aligned, pq_kv4_attention_workspace_bytes of the same arguments (at most 160 MiB).
+ * T * n_heads < 2^31.
+ */
+size_t pq_kv4_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages,
+                                        const pq_kv4_cache* cache);
+int pq_kv4_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* cu_q, const int32_t* kv_len,
+                     int32_t B, int32_t max_q, const int32_t* block_table, int32_t table_pages, const pq_kv4_cache* cache,
+                     const void* prefix_k_f16, const void* prefix_v_f16, int32_t n_prefix, float softmax_scale, int32_t causal,
+                     void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,6 +24,16 @@ PQ_OK, PQ_ERR_NULL, PQ_ERR_SHAPE, PQ_ERR_ALIGN, PQ_ERR_SCALE, PQ_ERR_WORKSPACE, 
 
 _i64, _i32, _f32, _vp, _sz = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
 
+
+
+class KV4Cache(ctypes.Structure):
+    """struct pq_kv4_cache."""
+    _fields_ = [("k_codes", _vp), ("v_codes", _vp), ("k_scale", _vp), ("v_scale", _vp), ("n_pages", _i64), ("n_kv_heads", _i32),
+                ("head_dim", _i32), ("page_size", _i32), ("group", _i32)]
+
+
+_cache = ctypes.POINTER(KV4Cache)
+
 # symbol -> (restype, argtypes); mirrors include/pq.h
 SIGNATURES = {
     "pq_version": (ctypes.c_int, []),
@@ -88,6 +98,11 @@ SIGNATURES = {
     "pq_calibrate_zp_workspace_bytes": (_sz, [_i64, _i32]),
     "pq_calibrate_static_zp": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _i32, _f32, _f32, _vp, _vp, _sz, _vp]),
     "pq_calibrate_static": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _i32, _f32, _vp, _vp, _sz, _vp]),
+    "pq_kv4_slots": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "pq_kv4_append": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _f32, _vp, _i64, _i32, _i32, _i32, _f32, _cache, _vp, _vp]),
+    "pq_kv4_attention_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32, _cache]),
+    "pq_kv4_attention": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _cache, _vp, _vp, _i32, _f32, _i32, _vp, _vp,
+                                        _sz, _vp]),
 }
 
 
@@ -665,6 +680,135 @@ def pq_calibrate_static_zp(x_cal, had_block: int, n_gamma: int = 8, n_beta: int 
                                         float(beta_min), _ptr(res), _ptr(ws), ws.numel(), _stream()),
            "pq_calibrate_static_zp")
     return res
+
+
+def pq_kv4_slots(kv_len, q_len, block_table, free_pages, page_size: int, T: int, taken=None, position_offset: int = 0, cu_q=None,
+                 kv_len_out=None, positions=None, slots=None, taken_out=None):
+    """Places for a step's new tokens: kv_len, q_len int32 [B], block_table int32 [B, pages] (new entries are written), free_pages int32,
+    taken int32 (pages of the list already given out; None = 0), T rows.
+    Returns (cu_q int32 [B + 1], kv_len_out int32 [B], positions int32 [T], slots int64 [T], taken_out int32 [1])."""
+    device = kv_len.device
+    B = kv_len.numel()
+    if cu_q is None:
+        cu_q = torch.empty((B + 1,), dtype=torch.int32, device=device)
+    if kv_len_out is None:
+        kv_len_out = torch.empty((B,), dtype=torch.int32, device=device)
+    if positions is None:
+        positions = torch.empty((T,), dtype=torch.int32, device=device)
+    if slots is None:
+        slots = torch.empty((T,), dtype=torch.int64, device=device)
+    if taken_out is None:
+        taken_out = torch.empty((1,), dtype=torch.int32, device=device)
+    for t, what in ((kv_len, "kv_len"), (q_len, "q_len"), (block_table, "block_table"), (free_pages, "free_pages"), (cu_q, "cu_q"),
+                    (kv_len_out, "kv_len_out"), (positions, "positions"), (taken_out, "taken_out")):
+        _dev(t, torch.int32, what)
+    _dev(slots, torch.int64, "slots")
+    if taken is not None:
+        _dev(taken, torch.int32, "taken")
+    if (q_len.numel() != B or block_table.dim() != 2 or block_table.shape[0] != B or cu_q.numel() < B + 1 or kv_len_out.numel() < B or
+            positions.numel() < T or slots.numel() < T or taken_out.numel() < 1 or (taken is not None and taken.numel() < 1)):
+        raise ValueError("shape mismatch")
+    _check(lib().pq_kv4_slots(_ptr(kv_len), _ptr(q_len), B, _ptr(block_table), block_table.shape[1], _ptr(free_pages), free_pages.numel(),
+                              _ptr(taken), int(page_size), int(T), int(position_offset), _ptr(cu_q), _ptr(kv_len_out), _ptr(positions),
+                              _ptr(slots), _ptr(taken_out), _stream()), "pq_kv4_slots")
+    return cu_q, kv_len_out, positions, slots, taken_out
+
+
+def _kv4_cache(k_codes, v_codes, k_scale, v_scale, group: int):
+    """The cache of one layer as the library takes it; sizes from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
+    _dev(k_codes, torch.uint8, "k_codes")
+    _dev(v_codes, torch.uint8, "v_codes")
+    _dev(k_scale, torch.float32, "k_scale")
+    _dev(v_scale, torch.float32, "v_scale")
+    if k_codes.dim() != 4 or v_codes.shape != k_codes.shape:
+        raise ValueError("shape mismatch")
+    n_pages, heads, page_size, half = k_codes.shape
+    steps = heads if group <= 0 else n_pages * heads * page_size * (2 * half // group)
+    if k_scale.numel() != steps or v_scale.numel() != steps:
+        raise ValueError("shape mismatch")
+    return KV4Cache(_ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale), n_pages, heads, 2 * half, page_size, int(group))
+
+
+def _rows(t: torch.Tensor, what: str):
+    """A matrix of fp16 rows, which may lie apart."""
+    if not t.is_cuda or t.dtype != torch.float16 or t.dim() != 2 or t.stride(1) != 1:
+        raise TypeError("%s must be a %s matrix with contiguous rows on the GPU" % (what, torch.float16))
+
+
+def pq_kv4_append(qkv, n_heads: int, positions, slots, k_codes, v_codes, k_scale, v_scale, q_weight=None, k_weight=None, eps: float = 1e-6,
+                  cos_sin=None, interleaved: bool = False, rotate: bool = True, group: int = 0, clip: float = 1.0, out=None):
+    """qkv fp16 [T, (n_heads + 2 kv heads) * head_dim] -> turned queries fp16 [T, n_heads * head_dim]; the codes of keys and values go to
+    their slots (int64 [T]) of the cache, with group > 0 their steps too.  cos_sin: fp32 [positions, rotary_dim] or None."""
+    cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
+    _rows(qkv, "qkv")
+    _dev(slots, torch.int64, "slots")
+    T, D = qkv.shape[0], cache.head_dim
+    if qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * D or slots.numel() != T:
+        raise ValueError("shape mismatch")
+    for w in (q_weight, k_weight):
+        if w is not None:
+            _dev(w, torch.float16, "weight")
+            if w.numel() != D:
+                raise ValueError("shape mismatch")
+    rd = 0
+    if cos_sin is not None:
+        _dev(cos_sin, torch.float32, "cos_sin")
+        _dev(positions, torch.int32, "positions")
+        if cos_sin.dim() != 2 or positions.numel() != T:
+            raise ValueError("shape mismatch")
+        rd = cos_sin.shape[1]
+    if out is None:
+        out = torch.empty((T, n_heads * D), dtype=torch.float16, device=qkv.device)
+    else:
+        _result(out, T * n_heads * D, "out")
+    _check(lib().pq_kv4_append(_ptr(qkv), qkv.stride(0) if T > 1 else qkv.shape[1], T, int(n_heads), _ptr(positions), _ptr(slots), _ptr(q_weight),
+                               _ptr(k_weight), float(eps), _ptr(cos_sin), 0 if cos_sin is None else cos_sin.shape[0], rd, int(bool(interleaved)),
+                               int(bool(rotate)), float(clip), cache, _ptr(out), _stream()), "pq_kv4_append")
+    return out
+
+
+def pq_kv4_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, k_codes) -> int:
+    """Scratch memory of pq_kv4_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
+    n_pages, heads, page_size, half = k_codes.shape
+    cache = KV4Cache(None, None, None, None, n_pages, heads, 2 * half, page_size, 0)
+    return int(lib().pq_kv4_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), cache))
+
+
+def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, group: int = 0,
+                     prefix_k=None, prefix_v=None, causal: bool = True, out=None, workspace=None):
+    """Attention of q fp16 [T, n_heads * head_dim] over the cache behind optional prefix tokens (fp16 [n, kv heads, head_dim]): rows
+    cu_q[b] .. cu_q[b + 1] are request b's, whose kv_len[b] tokens lie in the pages block_table[b].  Returns (out, workspace)."""
+    cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
+    _rows(q, "q")
+    _dev(cu_q, torch.int32, "cu_q")
+    _dev(kv_len, torch.int32, "kv_len")
+    _dev(block_table, torch.int32, "block_table")
+    T, D, B = q.shape[0], cache.head_dim, kv_len.numel()
+    n_heads = q.shape[1] // D
+    n_prefix = 0 if prefix_k is None else prefix_k.shape[0]
+    if q.shape[1] != n_heads * D or cu_q.numel() != B + 1 or block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("shape mismatch")
+    if (prefix_k is None) != (prefix_v is None):
+        raise ValueError("prefix_k and prefix_v come together")
+    if n_prefix:
+        for t, what in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+            _dev(t, torch.float16, what)
+            if tuple(t.shape) != (n_prefix, cache.n_kv_heads, D):
+                raise ValueError("shape mismatch")
+    W = block_table.shape[1]
+    if workspace is None:
+        need = int(lib().pq_kv4_attention_workspace_bytes(T, B, n_heads, int(max_q), W, cache))
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=q.device)
+    else:
+        _dev(workspace, torch.uint8, "workspace")
+    if out is None:
+        out = torch.zeros((T, n_heads * D), dtype=torch.float16, device=q.device)
+    else:
+        _result(out, T * n_heads * D, "out")
+    _check(lib().pq_kv4_attention(_ptr(q), q.stride(0) if T > 1 else q.shape[1], T, n_heads, _ptr(cu_q), _ptr(kv_len), B, int(max_q),
+                                  _ptr(block_table), W, cache, _ptr(prefix_k), _ptr(prefix_v), n_prefix, float(softmax_scale), int(bool(causal)),
+                                  _ptr(out), _ptr(workspace), workspace.numel(), _stream()), "pq_kv4_attention")
+    return out, workspace
 
 
 def pq_set_gemm_variant(variant: int) -> int:

@@ -1,0 +1,312 @@
+// A step's queries, keys and values on their way into attention: per-head RMS norm, position rotation and Hadamard rotation (App. B
+// "Online Rotation", R3) of queries and keys, and the 4-bit codes of keys and values in the slots of a paged cache (Table 1: per-head
+// static steps of O2, group-wise dynamic ones of O1), in one pass over the fused projection's output.
+//
+//     queries, keys:  y = x / sqrt(mean x^2 + eps) * w;   (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin);   z = H_D y / sqrt(D)
+//     values:         z = x
+//     queries leave as fp16(z); codes = clamp(round_half_even(z / step), -8, 7)
+//
+// The codes are those of the definition in double precision.  They are computed in fp32; where a quotient lies nearer to a border
+// k + 1/2 than the error of the fp32 path can reach, its head vector is computed again in fp64 (a few in a thousand), so neither the
+// order of the fp32 sums nor their contraction shows in the cache.
+//
+// Bound by HBM: 2 bytes of every channel in, 2 out for queries and half a byte for keys and values.  A lane holds eight channels
+// (16 bytes), D / 8 lanes a head, a wavefront the same head of 8 or 4 consecutive tokens: one kind of work to a wavefront, the step and
+// the norm's weights are read once, and in a page the tokens of a head lie one after another.  The four wavefronts of a workgroup take
+// four neighbouring heads of these tokens, which share the rows of the table of angles.
+#include "pq_kv4.h"
+#include "pq_rotate.h"
+
+namespace pq {
+namespace kv4 {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <int B> __device__ __forceinline__ float from_lane_xor(float v) { return rq::lane_xor<B>(v); }
+template <int B> __device__ __forceinline__ double from_lane_xor(double v) { return __shfl_xor(v, 1 << B, 64); }
+
+// Over the lanes of 2^BITS neighbours.
+template <int BITS, typename F> __device__ __forceinline__ F sum_lanes(F v)
+{
+    static_for<0, BITS>([&](auto B) { v += from_lane_xor<decltype(B)::value>(v); });
+    return v;
+}
+template <int BITS, typename F> __device__ __forceinline__ F max_lanes(F v)
+{
+    static_for<0, BITS>([&](auto B) { v = max(v, from_lane_xor<decltype(B)::value>(v)); });
+    return v;
+}
+
+// What a lane knows about its eight channels of a query or key, the same for the fp32 and the fp64 path.
+struct Lane {
+    float x[8];
+    float w[8];           // the norm's weight, or 1
+    float cs[8], sn[8];   // cosine and sine of each channel's angle, the sine with the sign it enters with; 1 and 0 where nothing turns
+    int partner;          // lane whose channels turn with this one's (halves), or -1: neighbouring channels turn
+};
+
+template <typename F, int LOG2_D, bool ROTATE>
+__device__ __forceinline__ void turn(const Lane& c, bool norm, bool rope, F eps, int lane, F (&v)[8])
+{
+    constexpr int kLaneBits = LOG2_D - 3;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (F)c.x[i];
+    if (norm) {
+        F sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i] * v[i];
+        sum = sum_lanes<kLaneBits>(sum);
+        const F mean = sum * (F)(1.0 / (1 << LOG2_D)) + eps;
+        F scale;
+        if constexpr (std::is_same<F, double>::value) scale = 1.0 / sqrt(mean);
+        else scale = __builtin_amdgcn_rsqf(mean);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= scale * (F)c.w[i];
+    }
+    if (rope) {
+        F other[8];
+        if (c.partner >= 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = __shfl(v[i], c.partner, 64);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = v[i ^ 1];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * (F)c.cs[i] + other[i] * (F)c.sn[i];
+    }
+    if constexpr (ROTATE) {
+        if constexpr (std::is_same<F, float>::value) {
+            rq::reg_stages8(v, 3);
+            static_for<0, kLaneBits>([&](auto B) { rq::lane_stage<decltype(B)::value>(v, lane); });
+            const float sign = rq::lane_sign(lane, kLaneBits);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= sign;
+        } else {
+            static_for<0, 3>([&](auto S) {
+                constexpr int d = 1 << decltype(S)::value;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if ((i & d) == 0) {
+                        const F a = v[i], b = v[i + d];
+                        v[i] = a + b;
+                        v[i + d] = a - b;
+                    }
+            });
+            static_for<0, kLaneBits>([&](auto B) {
+                constexpr int b = decltype(B)::value;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const F p = from_lane_xor<b>(v[i]);
+                    v[i] = (lane >> b) & 1 ? p - v[i] : p + v[i];
+                }
+            });
+        }
+    }
+}
+
+// Codes of eight quotients, and whether one of them is nearer than `near` to a border between two codes.
+__device__ __forceinline__ uint32_t codes8(const float (&t)[8], float near, bool& suspect)
+{
+    uint32_t s = 0;
+    suspect = false;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+        const float c = __builtin_amdgcn_fmed3f(t[i], -8.0f, 7.0f), r = c + rq::kMagic;
+        suspect |= fabsf(c - (r - rq::kMagic)) > 0.5f - near;
+        s = (s << 4) + __float_as_uint(r);
+    }
+    return (s - rq::kMagicSum) ^ 0x88888888u;
+}
+
+__device__ __forceinline__ uint32_t codes8(const double (&t)[8])
+{
+    uint32_t s = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) s = (s << 4) | ((uint32_t)(int)fmin(fmax(rint(t[i]), -8.0), 7.0) & 15u);
+    return s;
+}
+
+template <int LOG2_D, int LOG2_GROUP, bool ROTATE>
+__global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
+{
+    constexpr int D = 1 << LOG2_D, kLanes = D / 8, kTokens = 64 / kLanes, kLaneBits = LOG2_D - 3;
+    constexpr int kGroupBits = LOG2_GROUP ? LOG2_GROUP - 3 : kLaneBits;
+    const int lane = threadIdx.x & 63, c = lane & (kLanes - 1);
+    const int head = blockIdx.y * (kThreads / 64) + (threadIdx.x >> 6);
+    const int Hkv = a.cache.n_kv_heads;
+    if (head >= a.n_heads + 2 * Hkv) return;                             // whole wavefronts; nothing synchronises the workgroup
+    const int64_t t = (int64_t)blockIdx.x * kTokens + lane / kLanes, row = min(t, a.T - 1);
+    const int64_t slot = a.slots[row];
+    const bool live = t < a.T && slot >= 0 && slot < a.cache.n_pages << a.cache.log2_page;
+    if (__builtin_amdgcn_ballot_w64(live) == 0) return;
+    const bool is_query = head < a.n_heads, is_value = head >= a.n_heads + Hkv;
+
+    Lane ln;
+    const v4i raw = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(a.qkv + row * a.row_stride + (int64_t)head * D + 8 * c));
+    const bool norm = !is_value && (is_query ? a.q_weight : a.k_weight) != nullptr;
+    const bool rope = !is_value && a.cos_sin != nullptr;
+    if (norm) {
+        const v4i w = *reinterpret_cast<const v4i*>((is_query ? a.q_weight : a.k_weight) + 8 * c);
+        const __half2* h = reinterpret_cast<const __half2*>(&w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(h[i]);
+            ln.w[2 * i] = f.x;
+            ln.w[2 * i + 1] = f.y;
+        }
+    }
+    ln.partner = -1;
+    if (rope) {
+        const int half = a.rotary_dim / 2;
+        const int64_t position = min(max((int64_t)a.positions[row], (int64_t)0), a.max_positions - 1);
+        const float* cs = a.cos_sin + position * a.rotary_dim;
+        const bool turns = 8 * c < a.rotary_dim;
+        if (a.interleaved) {
+            const float4 x = *reinterpret_cast<const float4*>(cs + (turns ? 4 * c : 0)), y = *reinterpret_cast<const float4*>(cs + half + (turns ? 4 * c : 0));
+            const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                ln.cs[2 * i] = ln.cs[2 * i + 1] = turns ? xs[i] : 1.0f;
+                ln.sn[2 * i] = turns ? -ys[i] : 0.0f;
+                ln.sn[2 * i + 1] = turns ? ys[i] : 0.0f;
+            }
+        } else {
+            const bool first = 8 * c < half;
+            const int at = turns ? (first ? 8 * c : 8 * c - half) : 0;
+            ln.partner = turns ? (first ? lane + half / 8 : lane - half / 8) : lane;
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(cs + at + i), y = *reinterpret_cast<const float4*>(cs + half + at + i);
+                const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    ln.cs[i + k] = turns ? xs[k] : 1.0f;
+                    ln.sn[i + k] = turns ? (first ? -ys[k] : ys[k]) : 0.0f;
+                }
+            }
+        }
+    }
+    {
+        const __half2* h = reinterpret_cast<const __half2*>(&raw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(h[i]);
+            ln.x[2 * i] = f.x;
+            ln.x[2 * i + 1] = f.y;
+        }
+    }
+    constexpr double kInvSqrt = LOG2_D == 6 ? 0.125 : 0.08838834764831845;   // 1 / sqrt(D)
+    static_assert(LOG2_D == 6 || LOG2_D == 7, "heads of 64 or 128 channels");
+    const double unit = ROTATE && !is_value ? kInvSqrt : 1.0;
+
+    float v[8];
+    if (is_value) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = ln.x[i];
+    } else {
+        turn<float, LOG2_D, ROTATE>(ln, norm, rope, a.eps, lane, v);
+    }
+    if (is_query) {
+        const float m = (float)unit;
+        v4i o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 h = __floats2half2_rn(v[2 * i] * m, v[2 * i + 1] * m);
+            o[i] = *reinterpret_cast<const int*>(&h);
+        }
+        if (live) *reinterpret_cast<v4i*>(a.q_out + (t * a.n_heads + head) * D + 8 * c) = o;
+        return;
+    }
+
+    const int kv_head = head - a.n_heads - (is_value ? Hkv : 0);
+    const int64_t page = slot >> a.cache.log2_page, at = slot & ((1ll << a.cache.log2_page) - 1);
+    const int64_t token = (((page * Hkv + kv_head) << a.cache.log2_page) + at);   // of this head in the cache
+    float* const scales = is_value ? a.cache.v_scale : a.cache.k_scale;
+    float step;
+    if constexpr (LOG2_GROUP == 0) {
+        step = scales[kv_head];
+    } else {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
+        step = (float)((double)a.clip * ((double)max_lanes<kGroupBits>(most) * unit) / 7.0);
+        if (!(step > 0.0f)) step = 1.0f;
+    }
+    const float mult = (float)(unit / (double)step);
+    float t8[8], norm2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        t8[i] = v[i] * mult;
+        norm2 = fmaf(t8[i], t8[i], norm2);
+    }
+    // The reciprocal and its product are off by 2^-23 of a quotient, 2^-20 at the end of the range.  Norm, position rotation and
+    // butterflies are orthogonal up to a factor: each rounds by 2^-24 of the vector's length at most and passes on what came before, 12 such
+    // roundings in all, and the norm's factor itself is within 2^-21 of its value, 2^-18 at the end of the range.
+    float near = 0x1.0p-17f;
+    if (!is_value) near += 0x1.0p-20f * __builtin_amdgcn_sqrtf(sum_lanes<kLaneBits>(norm2));
+    bool suspect;
+    uint32_t codes = codes8(t8, near, suspect);
+    if (const uint64_t found = __builtin_amdgcn_ballot_w64(suspect && live); found != 0) {
+        double d[8];
+        if (is_value) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = (double)ln.x[i];
+        } else {
+            turn<double, LOG2_D, ROTATE>(ln, norm, rope, (double)a.eps, lane, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] *= unit;
+        }
+        float exact_step = step;
+        if constexpr (LOG2_GROUP != 0) {
+            double most = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmax(most, fabs(d[i]));
+            exact_step = (float)((double)a.clip * max_lanes<kGroupBits>(most) / 7.0);
+            if (!(exact_step > 0.0f)) exact_step = 1.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] /= (double)exact_step;
+        const uint32_t exact = codes8(d);
+        // only the vectors that asked for it: what a token gets does not depend on its neighbours
+        if ((found >> (lane & ~(kLanes - 1))) & ((1ull << kLanes) - 1)) {
+            codes = exact;
+            step = exact_step;
+        }
+    }
+    if (!live) return;
+    reinterpret_cast<uint32_t*>((is_value ? a.cache.v_codes : a.cache.k_codes) + token * (D / 2))[c] = codes;
+    if constexpr (LOG2_GROUP != 0) {
+        if ((c & ((1 << kGroupBits) - 1)) == 0) scales[token * (D >> LOG2_GROUP) + (c >> kGroupBits)] = step;
+    }
+}
+
+template <int LOG2_D, int LOG2_GROUP>
+int launch(const AppendArgs& a, bool rotate, hipStream_t st)
+{
+    constexpr int kTokens = 64 / ((1 << LOG2_D) / 8);
+    const int64_t blocks = (a.T + kTokens - 1) / kTokens;
+    const dim3 grid((unsigned)blocks, (unsigned)((a.n_heads + 2 * a.cache.n_kv_heads + 3) / 4));
+    if (rotate) k_kv4_append<LOG2_D, LOG2_GROUP, true><<<grid, kThreads, 0, st>>>(a);
+    else k_kv4_append<LOG2_D, LOG2_GROUP, false><<<grid, kThreads, 0, st>>>(a);
+    return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_append(const AppendArgs& a, int32_t head_dim, int32_t group, bool rotate, hipStream_t st)
+{
+    if (head_dim == 64) {
+        if (group == 0) return launch<6, 0>(a, rotate, st);
+        if (group == 32) return launch<6, 5>(a, rotate, st);
+        return launch<6, 6>(a, rotate, st);
+    }
+    if (group == 0) return launch<7, 0>(a, rotate, st);
+    if (group == 32) return launch<7, 5>(a, rotate, st);
+    if (group == 64) return launch<7, 6>(a, rotate, st);
+    return launch<7, 7>(a, rotate, st);
+}
+
+}  // namespace kv4
+}  // namespace pq

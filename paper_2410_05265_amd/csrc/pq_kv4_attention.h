@@ -1,0 +1,89 @@
+// What the attention kernels over the paged 4-bit cache share.
+//
+//     out_i = sum_t p_it v_t / sum_t p_it,    p_it = exp2(c k_t . q_i - m_i),    c = softmax_scale * log2(e)
+//
+// over the prefix tokens and the cached ones that query i sees (Eq. 3 of the paper: the prefix in full precision in front of the
+// quantized keys and values).  Scores are computed transposed, S^T = K Q^T: a lane then holds scores of one query, their maximum and sum
+// stay within the lane, and the probabilities lie in its registers as the second product O^T = V^T P^T wants them.
+//
+// Codes as fp16 operands: u = code + 8 (one exclusive or for eight) moved to bits 4 to 7 of each half is the subnormal number u * 2^-20,
+// which the matrix instructions take exactly: a mask and at most one shift for two codes, no subtraction.  The offset leaves by itself:
+// K (u - 8) q starts its sum at -8 sum(q) 2^-20, and sum p (u - 8) = sum p u - 8 sum p, where sum p is the softmax's own denominator (of
+// the rounded probabilities that the product uses).  (At bits 0 to 3 the products lose low bits against the accumulator: 6e-7 of the largest
+// sum, at bits 4 to 7 none were lost.)
+//
+// Probabilities are rounded to fp16 relative to a reference m that lags behind the running maximum: it moves only when a score passes it by
+// 14 (p <= 2^14), and then to 6 above which 2^6 = p stands.  p keeps fp16's full precision down to 2^-20 of the largest, the accumulators are
+// rescaled only when the reference moves, by a power of two, and the denominator sums what was rounded.
+#pragma once
+
+#include "pq_kv4.h"
+
+namespace pq {
+namespace kv4 {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+constexpr float kNothing = -1e30f;       // reference before the first score
+constexpr float kMost = 14.0f, kBack = 6.0f;
+constexpr float kUnit = 0x1.0p20f;       // a code as operand is u * 2^-20
+constexpr uint32_t kNibble = 0x00F000F0u, kOffset = 0x88888888u;
+
+// Codes j and j + 4 of a dword (already offset to 0..15) as two fp16 operands.
+template <int J> __device__ __forceinline__ uint32_t operand(uint32_t u)
+{
+    if constexpr (J == 0) return (u << 4) & kNibble;
+    else if constexpr (J == 1) return u & kNibble;
+    else if constexpr (J == 2) return (u >> 4) & kNibble;
+    else return (u >> 8) & kNibble;
+}
+
+// Eight codes of a key as an operand: channels in the order 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ v8h key_operand(uint32_t codes)
+{
+    const uint32_t u = codes ^ kOffset;
+    const v4u r = {operand<0>(u), operand<1>(u), operand<2>(u), operand<3>(u)};
+    return __builtin_bit_cast(v8h, r);
+}
+
+// Eight fp16 values in that order.
+__device__ __forceinline__ v8h in_key_order(const v4u d)
+{
+    const v4u r = {__builtin_amdgcn_perm(d[2], d[0], 0x05040100u), __builtin_amdgcn_perm(d[2], d[0], 0x07060302u),
+                   __builtin_amdgcn_perm(d[3], d[1], 0x05040100u), __builtin_amdgcn_perm(d[3], d[1], 0x07060302u)};
+    return __builtin_bit_cast(v8h, r);
+}
+
+__device__ __forceinline__ uint32_t two_halves(float a, float b)
+{
+    const v2h h = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, h);
+}
+
+__device__ __forceinline__ float add_halves(uint32_t pair, float to)
+{
+    const v2h one = {(_Float16)1.0f, (_Float16)1.0f};
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, pair), one, to, false);
+}
+
+// A request as the kernels see it: nothing that lies on the device takes them out of bounds.
+struct Request {
+    int32_t start, q_len, n;     // first row, rows, cached tokens
+};
+
+__device__ __forceinline__ Request request(const AttentionArgs& a, int b)
+{
+    Request r;
+    const int64_t from = min(max((int64_t)a.cu_q[b], (int64_t)0), a.T), to = min(max((int64_t)a.cu_q[b + 1], from), a.T);
+    r.start = (int32_t)from;
+    r.q_len = (int32_t)(to - from);
+    r.n = (int32_t)min((int64_t)max(a.kv_len[b], 0), (int64_t)a.table_pages << a.cache.log2_page);
+    return r;
+}
+
+}  // namespace kv4
+}  // namespace pq
