@@ -598,7 +598,7 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
  * q_f16     in  [T, n_heads * head_dim] fp16, rows row_stride values apart (a multiple of 8).
  * cu_q      in  int32 [B + 1], ascending;  kv_len: int32 [B], the new tokens included;  block_table: int32 [B, table_pages].
  *               kv_len is cut off at the table's pages; tokens of entries outside [0, n_pages) count as not seen.
- * max_q     the most queries of a request: a hint that chooses between kernels, results do not depend on it (>= 1).
+ * max_q     the most queries of a request: (>= 1) a hint that chooses between kernels: any value is right, and changes results in the order of sums alone.
  * prefix_k, prefix_v  in fp16 [n_prefix, n_kv_heads, head_dim] (rotated like the keys), NULL iff n_prefix = 0; n_prefix <= 1024.
  * out_f16   out [T, n_heads * head_dim] fp16; rows outside [cu_q[0], cu_q[B]) are left as they were; may not lie over q.
  * Scores, sums and the softmax's statistics are fp32; the probabilities are rounded to fp16 for the second product, and the sum that divides

@@ -64,7 +64,7 @@ int launch_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t
 int launch_append(const AppendArgs& a, int32_t head_dim, int32_t group, bool rotate, hipStream_t st);
 
 size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity);
-int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, void* ws, size_t ws_bytes, hipStream_t st);
+int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, void* ws, hipStream_t st);
 
 }  // namespace kv4
 }  // namespace pq

@@ -122,7 +122,7 @@ int pq_kv4_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n
                                       block_table, table_pages, c, static_cast<const __half*>(prefix_k_f16),
                                       static_cast<const __half*>(prefix_v_f16), n_prefix, softmax_scale, causal,
                                       static_cast<__half*>(out_f16)};
-    return pq::kv4::launch_attention(a, cache->head_dim, cache->group, max_q, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+    return pq::kv4::launch_attention(a, cache->head_dim, cache->group, max_q, workspace, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -28,6 +28,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
+constexpr int kTileRows = 256;           // rows of a workgroup of the kernel for many queries
+
 constexpr float kNothing = -1e30f;       // reference before the first score
 constexpr float kMost = 14.0f, kBack = 6.0f;
 constexpr float kUnit = 0x1.0p20f;       // a code as operand is u * 2^-20
@@ -84,6 +86,10 @@ __device__ __forceinline__ Request request(const AttentionArgs& a, int b)
     r.n = (int32_t)min((int64_t)max(a.kv_len[b], 0), (int64_t)a.table_pages << a.cache.log2_page);
     return r;
 }
+
+// Requests of more than small_rows rows (tokens times query heads of a key/value head); the others are the row kernel's.
+size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity);
+int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st);
 
 }  // namespace kv4
 }  // namespace pq

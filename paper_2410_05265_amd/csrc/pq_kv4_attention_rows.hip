@@ -26,10 +26,11 @@ constexpr float kLeast = 0x1.0p-80f;               // smallest reference of valu
 
 __device__ __forceinline__ int64_t units_of_tile(const Request& r) { return r.n > 0 ? (r.n + kUnitTokens - 1) / kUnitTokens : 1; }
 
-// Units of a request: (heads x tiles of rows) x units of its history.
-__device__ __forceinline__ int64_t units_of(const AttentionArgs& a, const Request& r, int& tiles)
+// Units of a request: (heads x tiles of rows) x units of its history; none if it has more than small_rows rows.
+__device__ __forceinline__ int64_t units_of(const AttentionArgs& a, const Request& r, int small_rows, int& tiles)
 {
-    tiles = (int)(((int64_t)r.q_len * a.heads_per_kv + kRows - 1) / kRows);
+    const int64_t rows = (int64_t)r.q_len * a.heads_per_kv;
+    tiles = rows > small_rows ? 0 : (int)((rows + kRows - 1) / kRows);
     return units_of_tile(r) * tiles * a.cache.n_kv_heads;
 }
 
@@ -40,7 +41,7 @@ struct Plan {
     int first, last;            // this lane's requests
 };
 
-__device__ __forceinline__ Plan plan(const AttentionArgs& a, int lane)
+__device__ __forceinline__ Plan plan(const AttentionArgs& a, int small_rows, int lane)
 {
     Plan p;
     const int each = (a.B + 63) / 64;
@@ -49,7 +50,7 @@ __device__ __forceinline__ Plan plan(const AttentionArgs& a, int lane)
     p.own = 0;
     for (int b = p.first; b < p.last; ++b) {
         int tiles;
-        p.own += units_of(a, request(a, b), tiles);
+        p.own += units_of(a, request(a, b), small_rows, tiles);
     }
     int64_t incl = p.own;
 #pragma unroll
@@ -77,7 +78,7 @@ struct Codes {
 };
 
 template <int D, int G, bool DYNAMIC>
-__global__ __launch_bounds__(kThreads, DYNAMIC ? 2 : 3) void k_kv4_attention_rows(AttentionArgs a, float* partial, int workers)
+__global__ __launch_bounds__(kThreads, DYNAMIC ? 2 : 3) void k_kv4_attention_rows(AttentionArgs a, float* partial, int workers, int small_rows)
 {
     constexpr int NG = D / G, KS = G / 32, CH = G / 16;
     typedef Codes<D, G, DYNAMIC> C;
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(kThreads, DYNAMIC ? 2 : 3) void k_kv4_attention_row
     const int col = lane & 15, quarter = lane >> 4;
     const int log2_page = a.cache.log2_page, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv;
 
-    const Plan p = plan(a, lane);
+    const Plan p = plan(a, small_rows, lane);
     const int64_t total = p.total;
     const int active = (int)min((int64_t)workers, total);
     const int worker = xcd_run(blockIdx.x, gridDim.x);
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(kThreads, DYNAMIC ? 2 : 3) void k_kv4_attention_row
         if (mine) {
             for (; at < p.last; ++at) {
                 int tiles;
-                const int64_t n = units_of(a, request(a, at), tiles);
+                const int64_t n = units_of(a, request(a, at), small_rows, tiles);
                 if (range < u + n) break;
                 u += n;
             }
@@ -115,8 +116,8 @@ __global__ __launch_bounds__(kThreads, DYNAMIC ? 2 : 3) void k_kv4_attention_row
     for (int64_t u0 = range; u0 < range_end;) {
         int tiles;
         const Request r = request(a, b);
-        const int64_t whole = units_of(a, r, tiles), per = units_of_tile(r);
-        if (u0 >= base + whole) {                  // (requests without queries have no units)
+        const int64_t whole = units_of(a, r, small_rows, tiles), per = units_of_tile(r);
+        if (u0 >= base + whole) {                  // (requests without queries, or with many, have no units)
             base += whole;
             ++b;
             continue;
@@ -472,14 +473,14 @@ __global__ __launch_bounds__(kThreads, DYNAMIC ? 2 : 3) void k_kv4_attention_row
 
 // Adds the partial sums of every row whose history was cut: one wavefront to a row and head.
 template <int D>
-__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, int workers)
+__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, int workers, int small_rows)
 {
     const int lane = threadIdx.x & 63;
     const int64_t index = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
     if (index >= a.T * a.n_heads) return;
     const int64_t at = index / a.n_heads;
     const int q_head = (int)(index % a.n_heads), head = q_head / a.heads_per_kv;
-    const Plan p = plan(a, lane);
+    const Plan p = plan(a, small_rows, lane);
     // the request that this row belongs to
     int b = -1;
     int64_t base = 0, u = p.before;
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
             b = i;
             base = u;
         }
-        u += units_of(a, r, tiles);
+        u += units_of(a, r, small_rows, tiles);
     }
     const uint64_t found = __builtin_amdgcn_ballot_w64(b >= 0);
     if (found == 0) return;
@@ -499,7 +500,8 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
     base = __shfl(base, from, 64);
     const Request r = request(a, b);
     int tiles;
-    units_of(a, r, tiles);
+    units_of(a, r, small_rows, tiles);
+    if (tiles == 0) return;
     const int64_t per = units_of_tile(r), total = p.total;
     const int row = (int)(at - r.start) * a.heads_per_kv + q_head % a.heads_per_kv;
     const int64_t first = base + ((int64_t)head * tiles + row / kRows) * per, last = first + per - 1;
@@ -528,10 +530,10 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
 }
 
 template <int D, int G, bool DYNAMIC>
-int launch(const AttentionArgs& a, int workers, float* partial, hipStream_t st)
+int launch(const AttentionArgs& a, int workers, int small_rows, float* partial, hipStream_t st)
 {
-    k_kv4_attention_rows<D, G, DYNAMIC><<<workers, kThreads, 0, st>>>(a, partial, workers);
-    k_kv4_attention_join<D><<<(unsigned)((a.T * a.n_heads + kWaves - 1) / kWaves), kThreads, 0, st>>>(a, partial, workers);
+    k_kv4_attention_rows<D, G, DYNAMIC><<<workers, kThreads, 0, st>>>(a, partial, workers, small_rows);
+    k_kv4_attention_join<D><<<(unsigned)((a.T * a.n_heads + kWaves - 1) / kWaves), kThreads, 0, st>>>(a, partial, workers, small_rows);
     return hip_status(hipGetLastError());
 }
 
@@ -541,26 +543,46 @@ int workers_for(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int64
     return (int)(units < kWorkers ? units : kWorkers);
 }
 
-}  // namespace
-
-size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t, int64_t capacity)
+size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity)
 {
-    return (size_t)workers_for(T, B, n_heads, n_kv_heads, capacity) * 2 * kRows * (head_dim + 4) * sizeof(float);
+    const size_t bytes = (size_t)workers_for(T, B, n_heads, n_kv_heads, capacity) * 2 * kRows * (head_dim + 4) * sizeof(float);
+    return (bytes + 255) & ~(size_t)255;
 }
 
-int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t, void* ws, size_t, hipStream_t st)
+int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st)
 {
     const int workers = workers_for(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
-    float* partial = static_cast<float*>(ws);
     if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false>(a, workers, partial, st);
-        if (group == 32) return launch<64, 32, true>(a, workers, partial, st);
-        return launch<64, 64, true>(a, workers, partial, st);
+        if (group == 0) return launch<64, 64, false>(a, workers, small_rows, partial, st);
+        if (group == 32) return launch<64, 32, true>(a, workers, small_rows, partial, st);
+        return launch<64, 64, true>(a, workers, small_rows, partial, st);
     }
-    if (group == 0) return launch<128, 128, false>(a, workers, partial, st);
-    if (group == 32) return launch<128, 32, true>(a, workers, partial, st);
-    if (group == 64) return launch<128, 64, true>(a, workers, partial, st);
-    return launch<128, 128, true>(a, workers, partial, st);
+    if (group == 0) return launch<128, 128, false>(a, workers, small_rows, partial, st);
+    if (group == 32) return launch<128, 32, true>(a, workers, small_rows, partial, st);
+    if (group == 64) return launch<128, 64, true>(a, workers, small_rows, partial, st);
+    return launch<128, 128, true>(a, workers, small_rows, partial, st);
+}
+
+// Requests of up to this many rows take the row kernel where the call may hold larger ones.
+constexpr int kSmallRows = 64;
+
+bool takes_tiles(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv > kSmallRows; }
+
+}  // namespace
+
+size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity)
+{
+    const size_t rows = rows_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, capacity);
+    return rows + (takes_tiles(max_q, n_heads / n_kv_heads) ? tiles_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, capacity) : 0);
+}
+
+int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, void* ws, hipStream_t st)
+{
+    float* const partial = static_cast<float*>(ws);
+    if (!takes_tiles(max_q, a.heads_per_kv)) return launch_rows(a, head_dim, group, INT32_MAX, partial, st);
+    const size_t rows = rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, (int64_t)a.table_pages << a.cache.log2_page);
+    const int rc = launch_attention_tiles(a, head_dim, group, kSmallRows, partial + rows / sizeof(float), st);
+    return rc == PQ_OK ? launch_rows(a, head_dim, group, kSmallRows, partial, st) : rc;
 }
 
 }  // namespace kv4
