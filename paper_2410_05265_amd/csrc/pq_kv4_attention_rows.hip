@@ -4,10 +4,11 @@
 // 16 or 32 of them (CB blocks of 16), so that up to as many read every code once.  Bound by HBM: 128 bytes of codes for a token and head of
 // 128 channels.
 //
-// Work is cut over the histories, in units of kUnitTokens tokens of one request, head and tile of rows.  All units of the call lie one after
-// another, and every workgroup takes an equal run of them, whatever the requests' lengths are: a run that covers a history whole writes
-// its outputs, one that begins or ends inside a history leaves a partial sum (at most two to a workgroup), and a second small kernel
-// adds those, in the order of the workgroups.  The lengths are read on the device, so a captured call follows them.
+// Work is cut over the histories, in units of kTile tokens of one request, head and tile of rows.  All units of the call lie one after another,
+// and every wavefront takes an equal run of them, whatever the requests' lengths are: a run that covers a history whole writes its outputs,
+// one that begins or ends inside a history leaves a partial sum (at most two to a wavefront), and a second small kernel adds those, in the
+// order of the wavefronts.  Wavefronts never wait for one another: with runs to a workgroup, and its four wavefronts' sums joined behind
+// barriers, the ends of histories cost a tenth of the time.  The lengths are read on the device, so a captured call follows them.
 //
 // A wavefront takes 32 tokens at a time.  Their codes go from memory straight into its ring of kDepth places in LDS, so three tiles are on
 // their way without a register; a lane then reads 16 bytes of a token's key codes (its part of every step of the first product), and 4
@@ -23,28 +24,31 @@ namespace {
 __device__ __forceinline__ v4f product(const v8h& a, const v8h& b, const v4f& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kTile = 32;                          // tokens of a wavefront's step
-constexpr int kUnitTokens = kTile * kWaves;
-constexpr int kDepth = 4;                          // places of a wavefront's ring
-constexpr int kWorkers = 512;                      // two workgroups to a CU, as their LDS allows
+constexpr int kTile = 32;                          // tokens of a wavefront's step: a unit
+constexpr int kLeastUnits = 2;                     // of a run, where there are fewer than wavefronts
 constexpr float kLeast = 0x1.0p-80f;               // smallest reference of value weights (dynamic steps)
 
-__device__ __forceinline__ int64_t units_of_tile(const Request& r) { return r.n > 0 ? (r.n + kUnitTokens - 1) / kUnitTokens : 1; }
+__device__ __forceinline__ int64_t units_of_tile(const Request& r) { return r.n > 0 ? (r.n + kTile - 1) / kTile : 1; }
 
-// Units of a request: (heads x tiles of rows) x units of its history; none if it has more than small_rows rows.
+// Histories of a request: heads x tiles of rows; none if it has more than small_rows rows.
 template <int ROWS>
-__device__ __forceinline__ int64_t units_of(const AttentionArgs& a, const Request& r, int small_rows, int& tiles)
+__device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r, int small_rows)
 {
     const int64_t rows = (int64_t)r.q_len * a.heads_per_kv;
-    tiles = rows > small_rows ? 0 : (int)((rows + ROWS - 1) / ROWS);
-    return units_of_tile(r) * tiles * a.cache.n_kv_heads;
+    return rows > small_rows ? 0 : (int)((rows + ROWS - 1) / ROWS);
 }
 
-// The requests' units: each lane of the calling wavefront sums a run of requests.
+__device__ __forceinline__ int64_t divided(int64_t x, int64_t by)
+{
+    if (((x | by) >> 32) == 0) return (uint32_t)x / (uint32_t)by;      // a third of the instructions
+    return x / by;
+}
+
+// The requests' histories and units: each lane of the calling wavefront sums a run of requests.
 struct Plan {
-    int64_t total, before;      // all units; those before this lane's requests
-    int64_t own;
-    int first, last;            // this lane's requests
+    int64_t total, before, own;          // units: all, those before this lane's requests, and theirs
+    int64_t items, items_before;         // histories
+    int first, last;                     // this lane's requests
 };
 
 template <int ROWS>
@@ -55,40 +59,34 @@ __device__ __forceinline__ Plan plan(const AttentionArgs& a, int small_rows, int
     p.first = min(lane * each, a.B);
     p.last = min(p.first + each, a.B);
     p.own = 0;
+    int64_t items = 0;
     for (int b = p.first; b < p.last; ++b) {
-        int tiles;
-        p.own += units_of<ROWS>(a, request(a, b), small_rows, tiles);
+        const Request r = request(a, b);
+        const int64_t n = (int64_t)tiles_of<ROWS>(a, r, small_rows) * a.cache.n_kv_heads;
+        items += n;
+        p.own += n * units_of_tile(r);
     }
-    int64_t incl = p.own;
+    int64_t units_incl = p.own, items_incl = items;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int64_t v = __shfl_up(incl, d, 64);
-        if (lane >= d) incl += v;
+        const int64_t u = __shfl_up(units_incl, d, 64), i = __shfl_up(items_incl, d, 64);
+        if (lane >= d) {
+            units_incl += u;
+            items_incl += i;
+        }
     }
-    p.before = incl - p.own;
-    p.total = __shfl(incl, 63, 64);
+    p.before = units_incl - p.own;
+    p.total = __shfl(units_incl, 63, 64);
+    p.items_before = items_incl - items;
+    p.items = __shfl(items_incl, 63, 64);
     return p;
 }
 
-// The request that unit u (below the total) belongs to, and its first unit.
-template <int ROWS>
-__device__ __forceinline__ int find_request(const AttentionArgs& a, const Plan& p, int small_rows, int64_t u, int64_t& base)
-{
-    const bool mine = p.before <= u && u < p.before + p.own;
-    int b = p.first;
-    int64_t first = p.before;
-    if (mine) {
-        for (; b < p.last; ++b) {
-            int tiles;
-            const int64_t n = units_of<ROWS>(a, request(a, b), small_rows, tiles);
-            if (u < first + n) break;
-            first += n;
-        }
-    }
-    const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine));
-    base = __shfl(first, from, 64);
-    return __builtin_amdgcn_readfirstlane(__shfl(b, from, 64));
-}
+// A history, as the kernel that adds partial sums takes it: `parts` wavefronts from `worker` on have some of it (one: it is done); the
+// first one's sum lies at its second place, if `second`.
+struct Item {
+    int worker, parts, second, start, rows, head, row0, unused;
+};
 
 // 16 or 4 bytes of every lane from memory straight into LDS, lane after lane from lds_addr (wavefront-uniform) on.
 __device__ __forceinline__ void to_lds16(const void* src, uint32_t lds_addr)
@@ -103,63 +101,91 @@ __device__ __forceinline__ void to_lds4(const void* src, uint32_t lds_addr)
 template <int D, int G, bool DYNAMIC, int CB>
 struct Shape {
     static constexpr int NG = D / G, KS = G / 32, CH = G / 16, ROWS = 16 * CB;
+    // Workgroups to a CU, and places of a wavefront's ring: what registers and LDS (160 KiB) allow.
+    static constexpr int PER_CU = CB == 1 && NG == 1 ? 3 : 2;
+    static constexpr int kDepth = PER_CU == 3 ? 3 : 4;
+    static constexpr int GROUPS = 256 * PER_CU;
     static constexpr int CODES = kTile * D / 2;                          // bytes of a tile's keys, and of its values
     static constexpr int SLOT = 2 * CODES + (DYNAMIC ? 256 * NG : 0);
     static constexpr int LOADS = 2 * CODES / 1024 + (DYNAMIC ? NG : 0);  // of a tile
-    static constexpr int PITCH = D + 4;                                  // floats of a row between the wavefronts' sums
-    static constexpr int RING = kWaves * kDepth * SLOT, SUMS = kWaves * ROWS * PITCH * 4;
-    static constexpr size_t kLds = (RING > SUMS ? RING : SUMS) + kWaves * ROWS * 8;
+    static constexpr size_t kLds = (size_t)kWaves * kDepth * SLOT;
 };
 
 template <int D, int G, bool DYNAMIC, int CB>
-__global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_rows(AttentionArgs a, float* partial, int workers, int small_rows)
+__global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void k_kv4_attention_rows(AttentionArgs a, float* partial, Item* items, int64_t most_items, int small_rows)
 {
     typedef Shape<D, G, DYNAMIC, CB> S;
-    constexpr int NG = S::NG, KS = S::KS, CH = S::CH, ROWS = S::ROWS;
+    constexpr int NG = S::NG, KS = S::KS, CH = S::CH, ROWS = S::ROWS, kDepth = S::kDepth;
     extern __shared__ __align__(256) uint8_t lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const int log2_page = a.cache.log2_page, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv;
-    float* const sums = reinterpret_cast<float*>(lds);                   // (over the rings)
-    float* const sum_m = reinterpret_cast<float*>(lds + S::kLds - kWaves * ROWS * 8);
-    float* const sum_l = sum_m + kWaves * ROWS;
     const uint8_t* const ring = lds + wave * kDepth * S::SLOT;
     const uint32_t ring_addr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)ring;
 
     const Plan p = plan<ROWS>(a, small_rows, lane);
-    const int64_t total = p.total;
-    const int active = (int)min((int64_t)workers, total);
-    const int worker = xcd_run(blockIdx.x, gridDim.x);
-    if (worker >= active) return;
-    const int64_t range = total * worker / active, range_end = total * (worker + 1) / active;
-    int64_t base;                                  // first unit of request b
-    int b = find_request<ROWS>(a, p, small_rows, range, base);
+    // (place 0 holds their count; only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
+    if (blockIdx.x == 0 && threadIdx.x == 0) items[0].parts = (int)min(p.items, most_items);
+    // the first `more` runs have one unit more
+    const int64_t workers = min((int64_t)gridDim.x * kWaves, (p.total + kLeastUnits - 1) / kLeastUnits);
+    const int worker = xcd_run(blockIdx.x, gridDim.x) * kWaves + wave;
+    if (worker >= workers) return;
+    const int64_t each = divided(p.total, workers), more = p.total - each * workers;
+    const int64_t range = each * worker + min((int64_t)worker, more), range_end = range + each + (worker < more ? 1 : 0);
+    auto worker_of = [&](int64_t unit) PQ_INLINE {
+        return unit < more * (each + 1) ? divided(unit, each + 1) : more + divided(unit - more * (each + 1), each);
+    };
+
+    // the request that the run begins in, its first unit and its first history
+    int b;
+    int64_t base, item_base;
+    {
+        const bool mine = p.before <= range && range < p.before + p.own;
+        int at = p.first;
+        int64_t u = p.before, i = p.items_before;
+        if (mine) {
+            for (; at < p.last; ++at) {
+                const Request r = request(a, at);
+                const int64_t n = (int64_t)tiles_of<ROWS>(a, r, small_rows) * Hkv;
+                if (range < u + n * units_of_tile(r)) break;
+                u += n * units_of_tile(r);
+                i += n;
+            }
+        }
+        const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine));
+        b = __builtin_amdgcn_readfirstlane(__shfl(at, from, 64));
+        base = __shfl(u, from, 64);
+        item_base = __shfl(i, from, 64);
+    }
 
     for (int64_t u0 = range; u0 < range_end;) {
-        int tiles;
         const Request r = request(a, b);
-        const int64_t whole = units_of<ROWS>(a, r, small_rows, tiles), per = units_of_tile(r);
+        const int tiles = tiles_of<ROWS>(a, r, small_rows);
+        const int64_t per = units_of_tile(r), whole = per * tiles * Hkv;
         if (u0 >= base + whole) {                  // (requests without queries, or with many, have no units)
             base += whole;
+            item_base += (int64_t)tiles * Hkv;
             ++b;
             continue;
         }
-        const int64_t item = (u0 - base) / per, from_unit = (u0 - base) % per, take = min(range_end - u0, per - from_unit);
-        const int head = __builtin_amdgcn_readfirstlane((int)(item / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(item % tiles));
+        const int64_t item = divided(u0 - base, per), from_unit = u0 - base - item * per, take = min(range_end - u0, per - from_unit);
+        const int head = __builtin_amdgcn_readfirstlane((int)item / tiles), tile = __builtin_amdgcn_readfirstlane((int)item % tiles);
         const int rows = r.q_len * per_kv;
         const int first_token = tile * ROWS / per_kv, last_token = min((tile * ROWS + ROWS - 1) / per_kv, r.q_len - 1);
         const int all_see = a.causal ? r.n - (r.q_len - 1 - first_token) : r.n;         // tokens before this one need no mask
         const int any_sees = a.causal ? r.n - (r.q_len - 1 - last_token) : r.n;
-        const int from = (int)(from_unit * kUnitTokens), to = (int)min((from_unit + take) * kUnitTokens, (int64_t)max(any_sees, 0));
+        const int from = (int)(from_unit * kTile), to = (int)min((from_unit + take) * kTile, (int64_t)max(any_sees, 0));
+        if (from_unit == 0 && lane == 0 && item_base + item < most_items)
+            items[1 + item_base + item] = {worker, take == per ? 1 : (int)worker_of(u0 + per - 1) - worker + 1, u0 == range ? 0 : 1, r.start, rows, head,
+                                           tile * ROWS, 0};
 
-        // ---- codes on their way: this wavefront's tiles are from + 32 wave + 128 i
+        // ---- codes on their way
         const int32_t* table = a.table + (int64_t)b * a.table_pages;
         int ids_from = -64, ids = 0;
-        const int t_first = from + wave * kTile;
-        const int count = __builtin_amdgcn_readfirstlane(t_first < to ? (to - t_first + kUnitTokens - 1) / kUnitTokens : 0);
+        const int count = __builtin_amdgcn_readfirstlane(from < to ? (to - from + kTile - 1) / kTile : 0);
         uint32_t bad_bits = 0;                     // two bits for each place of the ring: blocks of 16 tokens whose page is none
         auto fetch = [&](int i) PQ_INLINE {
-            const int t0 = t_first + i * kUnitTokens, place = i % kDepth;
+            const int t0 = from + i * kTile, place = i % kDepth;
             int64_t first[2];                      // of the blocks, in this head's part of the cache
             bad_bits &= ~(3u << (2 * place));
 #pragma unroll
@@ -195,8 +221,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_rows(AttentionArg
                 }
             }
         };
-        const bool prefix = a.n_prefix > 0 && from_unit == 0 && wave == 0;
-        const int early = prefix ? kDepth / 2 : kDepth;    // (the prefix tokens' values take the other places)
+        const bool prefix = a.n_prefix > 0 && from_unit == 0;
+        const int early = prefix ? kDepth - 2 : kDepth;    // (the prefix tokens' values take the other two places)
         for (int i = 0; i < min(count, early); ++i) fetch(i);
 
         // ---- queries: channels as the keys' operands have them
@@ -280,11 +306,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_rows(AttentionArg
             }
         };
 
-        // ---- prefix tokens, by the first wavefront of the run that begins the history
+        // ---- prefix tokens, by the run that begins the history
         if (prefix) {
-            const uint32_t to_addr = ring_addr + kDepth / 2 * S::SLOT;
-            const __half* const values = reinterpret_cast<const __half*>(ring + kDepth / 2 * S::SLOT);
-            static_assert(kDepth / 2 * S::SLOT >= kTile * D * 2, "32 tokens in fp16");
+            const uint32_t to_addr = ring_addr + (kDepth - 2) * S::SLOT;
+            const __half* const values = reinterpret_cast<const __half*>(ring + (kDepth - 2) * S::SLOT);
+            static_assert(2 * S::SLOT >= kTile * D * 2, "32 tokens in fp16");
             for (int t0 = 0; t0 < a.n_prefix; t0 += kTile) {
 #pragma unroll
                 for (int i = 0; i < kTile * D * 2 / 1024; ++i) {
@@ -347,10 +373,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_rows(AttentionArg
 
         // ---- the history
         for (int i = 0; i < count; ++i) {
-            const int t0 = t_first + i * kUnitTokens, place = i % kDepth;
+            const int t0 = from + i * kTile, place = i % kDepth;
             // until this tile is there; those behind it may be on their way
             const int behind = min(count - 1 - i, kDepth - 1);
-            if (behind == kDepth - 1) wait_vm<(kDepth - 1) * S::LOADS>();
+            if (behind == 3) wait_vm<3 * S::LOADS>();
             else if (behind == 2) wait_vm<2 * S::LOADS>();
             else if (behind == 1) wait_vm<S::LOADS>();
             else wait_vm<0>();
@@ -492,167 +518,171 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_rows(AttentionArg
             }
         }
 
-        // ---- the four wavefronts' sums become one
-        __syncthreads();                           // (they lie over the rings)
+        // ---- results.  Block j of a group holds channels CH * row + j: a lane's rows 4 quarter .. + 3 are 4 CH channels in a row.
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             l[c] += __shfl_xor(l[c], 16, 64);
             l[c] += __shfl_xor(l[c], 32, 64);
-            if (quarter == 0) {
-                sum_m[wave * ROWS + 16 * c + col] = m[c];
-                sum_l[wave * ROWS + 16 * c + col] = l[c];
-            }
-            const bool live = tile * ROWS + 16 * c + col < rows;
-            float* const dst = sums + (wave * ROWS + 16 * c + col) * S::PITCH;
+            const int row = tile * ROWS + 16 * c + col;
+            const bool live = row < rows;
+            const float f = take == per ? (l[c] > 0.0f ? v_step / l[c] : 0.0f) : v_step;
+            float* const part = partial + (((int64_t)worker * 2 + (u0 == range ? 0 : 1)) * ROWS + 16 * c + col) * (D + 4);
+            __half* const dst = a.out + ((int64_t)(r.start + min(row, rows - 1) / per_kv) * a.n_heads + head * per_kv + min(row, rows - 1) % per_kv) * D;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                float times = kUnit, minus = 8.0f * l[c];
+                float times = kUnit * f, minus = 8.0f * l[c] * f;
                 if constexpr (DYNAMIC) {
                     float lw_all = lw[c][g] + __shfl_xor(lw[c][g], 16, 64);
                     lw_all += __shfl_xor(lw_all, 32, 64);
-                    times = kUnit * ref[c][g];
-                    minus = 8.0f * lw_all * ref[c][g];
+                    times = kUnit * ref[c][g] * f;
+                    minus = 8.0f * lw_all * ref[c][g] * f;
                 }
-                // block j of a group holds channels CH * row + j: a lane's rows 4 quarter .. + 3 are 4 CH channels in a row
-                if (live) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < CH; ++j) dst[g * G + CH * (4 * quarter + i) + j] = fmaf(o[c][g * CH + j][i], times, -minus);
-                }
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-            constexpr int kEach = D / 16;
-            const int out_row = 16 * c + (tid >> 4), d0 = (tid & 15) * kEach, at_row = tile * ROWS + out_row;
-            if (at_row < rows) {
-                float top = sum_m[out_row], sum = 0.0f, acc[kEach];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sum_m[w * ROWS + out_row]);
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) acc[i] = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(sum_m[w * ROWS + out_row] - top);
-                    sum = fmaf(sum_l[w * ROWS + out_row], f, sum);
-#pragma unroll
-                    for (int i = 0; i < kEach; ++i) acc[i] = fmaf(sums[(w * ROWS + out_row) * S::PITCH + d0 + i], f * v_step, acc[i]);
-                }
+                const int ch = g * G + 4 * CH * quarter;
+                if (!live) continue;
                 if (take == per) {
-                    const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
-                    __half* dst = a.out + ((int64_t)(r.start + at_row / per_kv) * a.n_heads + head * per_kv + at_row % per_kv) * D + d0;
 #pragma unroll
-                    for (int i = 0; i < kEach; i += 2) *reinterpret_cast<__half2*>(dst + i) = __floats2half2_rn(acc[i] * f, acc[i + 1] * f);
+                    for (int i = 0; i < 4 * CH; i += 8) {
+                        v4u w;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            w[j] = two_halves(fmaf(o[c][g * CH + (i + 2 * j) % CH][(i + 2 * j) / CH], times, -minus),
+                                              fmaf(o[c][g * CH + (i + 2 * j + 1) % CH][(i + 2 * j + 1) / CH], times, -minus));
+                        *reinterpret_cast<v4u*>(dst + ch + i) = w;
+                    }
                 } else {
-                    const int64_t slot = (int64_t)worker * 2 + (u0 == range ? 0 : 1);
-                    float* dst = partial + (slot * ROWS + out_row) * (D + 4);
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i) dst[4 + d0 + i] = acc[i];
-                    if (d0 == 0) {
-                        dst[0] = top;
-                        dst[1] = sum;
+                    for (int i = 0; i < 4 * CH; i += 4) {
+                        v4f w;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = fmaf(o[c][g * CH + (i + j) % CH][(i + j) / CH], times, -minus);
+                        *reinterpret_cast<v4f*>(part + 4 + ch + i) = w;
                     }
                 }
             }
+            if (live && take != per && quarter == 0) {
+                part[0] = m[c];
+                part[1] = l[c];
+            }
         }
-        __syncthreads();
         u0 += take;
     }
 }
 
-// Adds the partial sums of the histories that were cut: a workgroup takes the one that the border before its worker's run is the first to cut.
+// Adds the partial sums of the histories that were cut: a workgroup takes four rows of one, one to a wavefront.
 template <int D, int CB>
-__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, int workers, int small_rows)
+__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items)
 {
-    constexpr int ROWS = 16 * CB, kEach = D / 16;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const Plan p = plan<ROWS>(a, small_rows, lane);
-    const int64_t total = p.total;
-    const int active = (int)min((int64_t)workers, total), worker = blockIdx.x + 1;
-    if (worker >= active) return;
-    auto start_of = [&](int w) { return total * w / active; };
-    const int64_t border = start_of(worker);
-    int64_t base;
-    const int b = find_request<ROWS>(a, p, small_rows, border, base);
-    const Request r = request(a, b);
-    int tiles;
-    units_of<ROWS>(a, r, small_rows, tiles);
-    const int64_t per = units_of_tile(r), item = (border - base) / per, first = base + item * per, last = first + per;
-    if (first == border || first < start_of(worker - 1)) return;       // not cut here, or by an earlier border as well
-    const int head = (int)(item / tiles), tile = (int)(item % tiles), rows = r.q_len * a.heads_per_kv;
+    constexpr int ROWS = 16 * CB, kEach = D / 64, kAtOnce = 8;
+    const int lane = threadIdx.x & 63, row = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int count = items[0].parts;
+    const Item item = items[1 + blockIdx.x];                             // (of the last call, or nothing, from the count on)
+    if (blockIdx.x >= count || item.parts <= 1 || item.row0 + row >= item.rows) return;
+    float top = kNothing, sum = 0.0f, acc[kEach];
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        const int row = 16 * c + (tid >> 4), d0 = (tid & 15) * kEach, at_row = tile * ROWS + row;
-        if (at_row >= rows) continue;
-        float top = kNothing, sum = 0.0f, acc[kEach];
+    for (int i = 0; i < kEach; ++i) acc[i] = 0.0f;
+    const float* const first = partial + ((int64_t)item.worker * 2 * ROWS + row) * (D + 4);
+    const int64_t step = 2 * ROWS * (D + 4), second = item.second ? ROWS * (D + 4) : 0;
+    for (int n0 = 0; n0 < item.parts; n0 += 64) {
+        const int n = min(item.parts - n0, 64), mine = n0 + min(lane, n - 1);
+        const float* const head = first + mine * step + (mine == 0 ? second : 0);
+        const float m = lane < n ? head[0] : kNothing, l = lane < n ? head[1] : 0.0f;
+        float to = m;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) acc[i] = 0.0f;
-        for (int w = worker - 1; w < active && start_of(w) < last; ++w) {
-            const int64_t slot = (int64_t)w * 2 + (start_of(w) >= first ? 0 : 1);
-            const float* src = partial + (slot * ROWS + row) * (D + 4);
-            const float m = src[0], to = fmaxf(top, m);
-            const float f = __builtin_amdgcn_exp2f(top - to), g = __builtin_amdgcn_exp2f(m - to);
-            sum = fmaf(sum, f, src[1] * g);
+        for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d, 64));
+        to = fmaxf(to, top);
+        const float old = __builtin_amdgcn_exp2f(top - to), f = __builtin_amdgcn_exp2f(m - to);
+        float part = lane < n ? l * f : 0.0f;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) acc[i] = fmaf(acc[i], f, src[4 + d0 + i] * g);
-            top = to;
+        for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d, 64);
+        sum = fmaf(sum, old, part);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) acc[i] *= old;
+        for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+            float x[kAtOnce][kEach];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int at = n0 + min(i0 + i, n - 1);
+                const float* src = first + at * step + (at == 0 ? second : 0) + 4 + kEach * lane;
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) x[i][k] = src[k];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const float fi = __shfl(f, min(i0 + i, n - 1), 64);
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) acc[k] = fmaf(x[i][k], i0 + i < n ? fi : 0.0f, acc[k]);
+            }
         }
-        const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
-        __half* dst = a.out + ((int64_t)(r.start + at_row / a.heads_per_kv) * a.n_heads + head * a.heads_per_kv + at_row % a.heads_per_kv) * D + d0;
-#pragma unroll
-        for (int i = 0; i < kEach; i += 2) *reinterpret_cast<__half2*>(dst + i) = __floats2half2_rn(acc[i] * f, acc[i + 1] * f);
+        top = to;
     }
+    const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const int at_row = item.row0 + row, per_kv = a.heads_per_kv;
+    __half* dst = a.out + ((int64_t)(item.start + at_row / per_kv) * a.n_heads + item.head * per_kv + at_row % per_kv) * D + kEach * lane;
+    if constexpr (kEach == 2) *reinterpret_cast<__half2*>(dst) = __floats2half2_rn(acc[0] * f, acc[1] * f);
+    else *dst = __float2half_rn(acc[0] * f);
+}
+
+// What a call has at most: histories (of 16 rows), and workgroups with something to do.
+struct Most {
+    int64_t items, groups;
+};
+Most at_most(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int64_t capacity, int small_rows)
+{
+    const int64_t by_rows = T * (n_heads / n_kv_heads) / 16 + B, by_requests = ((int64_t)small_rows + 15) / 16 * B;
+    const int64_t items = (by_rows < by_requests ? by_rows : by_requests) * n_kv_heads, units = items * ((capacity + kTile - 1) / kTile);
+    return {items, (units + kLeastUnits * kWaves - 1) / (kLeastUnits * kWaves)};
+}
+
+// Scratch memory: partial sums, two to a wavefront, then the list of histories.
+size_t partial_bytes(int64_t groups, int32_t head_dim, int blocks)
+{
+    return (size_t)(groups < 768 ? groups : 768) * kWaves * 2 * 16 * blocks * (head_dim + 4) * sizeof(float);
 }
 
 template <int D, int G, bool DYNAMIC, int CB>
-int launch(const AttentionArgs& a, int workers, int small_rows, float* partial, hipStream_t st)
+int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
 {
     static std::atomic<uint64_t> allowed{0};
     constexpr size_t lds = Shape<D, G, DYNAMIC, CB>::kLds;
     const auto kernel = k_kv4_attention_rows<D, G, DYNAMIC, CB>;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, allowed); rc != PQ_OK) return rc;
-    kernel<<<workers, kThreads, lds, st>>>(a, partial, workers, small_rows);
-    if (workers > 1) k_kv4_attention_join<D, CB><<<workers - 1, kThreads, 0, st>>>(a, partial, workers, small_rows);
+    const Most most = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page, small_rows);
+    const int64_t groups = most.groups < Shape<D, G, DYNAMIC, CB>::GROUPS ? most.groups : Shape<D, G, DYNAMIC, CB>::GROUPS;
+    float* const partial = static_cast<float*>(ws);
+    Item* const items = reinterpret_cast<Item*>(static_cast<uint8_t*>(ws) + partial_bytes(most.groups, D, CB));
+    kernel<<<(unsigned)groups, kThreads, lds, st>>>(a, partial, items, most.items, small_rows);
+    k_kv4_attention_join<D, CB><<<dim3((unsigned)most.items, 4 * CB), kThreads, 0, st>>>(a, partial, items);
     return hip_status(hipGetLastError());
-}
-
-// As many as the call can have units at most (tiles of 16 rows), up to the GPU's places.
-int workers_for(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int64_t capacity)
-{
-    const int64_t tiles = T * (n_heads / n_kv_heads) / 16 + B, units = tiles * n_kv_heads * ((capacity + kUnitTokens - 1) / kUnitTokens);
-    return (int)(units < kWorkers ? units : kWorkers);
 }
 
 // Column blocks: one, if it holds every request's rows (max_q is right, or more tiles of rows are taken).
 int blocks_for(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv <= 16 ? 1 : 2; }
 
-size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity)
-{
-    const size_t rows = (size_t)workers_for(T, B, n_heads, n_kv_heads, capacity) * 2 * 16 * blocks_for(max_q, n_heads / n_kv_heads);
-    return (rows * (head_dim + 4) * sizeof(float) + 255) & ~(size_t)255;
-}
-
-template <int CB>
-int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st)
-{
-    const int workers = workers_for(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
-    if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false, CB>(a, workers, small_rows, partial, st);
-        if (group == 32) return launch<64, 32, true, CB>(a, workers, small_rows, partial, st);
-        return launch<64, 64, true, CB>(a, workers, small_rows, partial, st);
-    }
-    if (group == 0) return launch<128, 128, false, CB>(a, workers, small_rows, partial, st);
-    if (group == 32) return launch<128, 32, true, CB>(a, workers, small_rows, partial, st);
-    if (group == 64) return launch<128, 64, true, CB>(a, workers, small_rows, partial, st);
-    return launch<128, 128, true, CB>(a, workers, small_rows, partial, st);
-}
-
-// Requests of up to this many rows take the row kernel where the call may hold larger ones.
+// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and this one the others.
 constexpr int kSmallRows = 64;
 
 bool takes_tiles(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv > kSmallRows; }
+int small_rows_for(int32_t max_q, int32_t per_kv) { return takes_tiles(max_q, per_kv) ? kSmallRows : INT32_MAX; }
+
+size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity)
+{
+    const Most most = at_most(T, B, n_heads, n_kv_heads, capacity, small_rows_for(max_q, n_heads / n_kv_heads));
+    return (partial_bytes(most.groups, head_dim, blocks_for(max_q, n_heads / n_kv_heads)) + (size_t)(most.items + 1) * sizeof(Item) + 255) & ~(size_t)255;
+}
+
+template <int CB>
+int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, void* ws, hipStream_t st)
+{
+    if (head_dim == 64) {
+        if (group == 0) return launch<64, 64, false, CB>(a, small_rows, ws, st);
+        if (group == 32) return launch<64, 32, true, CB>(a, small_rows, ws, st);
+        return launch<64, 64, true, CB>(a, small_rows, ws, st);
+    }
+    if (group == 0) return launch<128, 128, false, CB>(a, small_rows, ws, st);
+    if (group == 32) return launch<128, 32, true, CB>(a, small_rows, ws, st);
+    if (group == 64) return launch<128, 64, true, CB>(a, small_rows, ws, st);
+    return launch<128, 128, true, CB>(a, small_rows, ws, st);
+}
 
 }  // namespace
 
@@ -664,15 +694,14 @@ size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t 
 
 int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, void* ws, hipStream_t st)
 {
-    float* const partial = static_cast<float*>(ws);
-    const bool tiles = takes_tiles(max_q, a.heads_per_kv);
-    const int small_rows = tiles ? kSmallRows : INT32_MAX;
-    if (tiles) {
+    const int small_rows = small_rows_for(max_q, a.heads_per_kv);
+    if (takes_tiles(max_q, a.heads_per_kv)) {
         const size_t rows = rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, (int64_t)a.table_pages << a.cache.log2_page);
-        if (const int rc = launch_attention_tiles(a, head_dim, group, small_rows, partial + rows / sizeof(float), st); rc != PQ_OK) return rc;
+        float* const partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + rows);
+        if (const int rc = launch_attention_tiles(a, head_dim, group, small_rows, partial, st); rc != PQ_OK) return rc;
     }
-    return blocks_for(max_q, a.heads_per_kv) == 1 ? launch_rows<1>(a, head_dim, group, small_rows, partial, st)
-                                                  : launch_rows<2>(a, head_dim, group, small_rows, partial, st);
+    return blocks_for(max_q, a.heads_per_kv) == 1 ? launch_rows<1>(a, head_dim, group, small_rows, ws, st)
+                                                  : launch_rows<2>(a, head_dim, group, small_rows, ws, st);
 }
 
 }  // namespace kv4
