@@ -25,7 +25,10 @@ __device__ __forceinline__ v4f product(const v8h& a, const v8h& b, const v4f& c)
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kTile = 32;                          // tokens of a wavefront's step: a unit
-constexpr int kLeastUnits = 2;                     // of a run, where there are fewer than wavefronts
+constexpr int kDepth = 4;                          // places of a wavefront's ring
+// Two workgroups to a CU: 128 of its 160 KiB of LDS.  (Three with three places, where the registers allow them: 64 requests of up to 8192
+// tokens 84.1 us against 82.4, 24 x 32 heads of up to 2300 42.5 against 43.4, 3 requests of up to 131072 93.8 against 86.4.)
+constexpr int kPerCu = 2, kGroups = 256 * kPerCu;
 constexpr float kLeast = 0x1.0p-80f;               // smallest reference of value weights (dynamic steps)
 
 __device__ __forceinline__ int64_t units_of_tile(const Request& r) { return r.n > 0 ? (r.n + kTile - 1) / kTile : 1; }
@@ -49,6 +52,7 @@ struct Plan {
     int64_t total, before, own;          // units: all, those before this lane's requests, and theirs
     int64_t items, items_before;         // histories
     int first, last;                     // this lane's requests
+    Request r;                           // the last of them
 };
 
 template <int ROWS>
@@ -59,12 +63,13 @@ __device__ __forceinline__ Plan plan(const AttentionArgs& a, int small_rows, int
     p.first = min(lane * each, a.B);
     p.last = min(p.first + each, a.B);
     p.own = 0;
+    p.r = {0, 0, 0};
     int64_t items = 0;
     for (int b = p.first; b < p.last; ++b) {
-        const Request r = request(a, b);
-        const int64_t n = (int64_t)tiles_of<ROWS>(a, r, small_rows) * a.cache.n_kv_heads;
+        p.r = request(a, b);
+        const int64_t n = (int64_t)tiles_of<ROWS>(a, p.r, small_rows) * a.cache.n_kv_heads;
         items += n;
-        p.own += n * units_of_tile(r);
+        p.own += n * units_of_tile(p.r);
     }
     int64_t units_incl = p.own, items_incl = items;
 #pragma unroll
@@ -101,10 +106,6 @@ __device__ __forceinline__ void to_lds4(const void* src, uint32_t lds_addr)
 template <int D, int G, bool DYNAMIC, int CB>
 struct Shape {
     static constexpr int NG = D / G, KS = G / 32, CH = G / 16, ROWS = 16 * CB;
-    // Workgroups to a CU, and places of a wavefront's ring: what registers and LDS (160 KiB) allow.
-    static constexpr int PER_CU = CB == 1 && NG == 1 ? 3 : 2;
-    static constexpr int kDepth = PER_CU == 3 ? 3 : 4;
-    static constexpr int GROUPS = 256 * PER_CU;
     static constexpr int CODES = kTile * D / 2;                          // bytes of a tile's keys, and of its values
     static constexpr int SLOT = 2 * CODES + (DYNAMIC ? 256 * NG : 0);
     static constexpr int LOADS = 2 * CODES / 1024 + (DYNAMIC ? NG : 0);  // of a tile
@@ -112,10 +113,10 @@ struct Shape {
 };
 
 template <int D, int G, bool DYNAMIC, int CB>
-__global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void k_kv4_attention_rows(AttentionArgs a, float* partial, Item* items, int64_t most_items, int small_rows)
+__global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(AttentionArgs a, float* partial, Item* items, int64_t most_items, int small_rows)
 {
     typedef Shape<D, G, DYNAMIC, CB> S;
-    constexpr int NG = S::NG, KS = S::KS, CH = S::CH, ROWS = S::ROWS, kDepth = S::kDepth;
+    constexpr int NG = S::NG, KS = S::KS, CH = S::CH, ROWS = S::ROWS;
     extern __shared__ __align__(256) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void 
     // (place 0 holds their count; only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
     if (blockIdx.x == 0 && threadIdx.x == 0) items[0].parts = (int)min(p.items, most_items);
     // the first `more` runs have one unit more
-    const int64_t workers = min((int64_t)gridDim.x * kWaves, (p.total + kLeastUnits - 1) / kLeastUnits);
+    const int64_t workers = min((int64_t)gridDim.x * kWaves, p.total);
     const int worker = xcd_run(blockIdx.x, gridDim.x) * kWaves + wave;
     if (worker >= workers) return;
     const int64_t each = divided(p.total, workers), more = p.total - each * workers;
@@ -139,13 +140,15 @@ __global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void 
     // the request that the run begins in, its first unit and its first history
     int b;
     int64_t base, item_base;
+    Request r;
     {
         const bool mine = p.before <= range && range < p.before + p.own;
         int at = p.first;
         int64_t u = p.before, i = p.items_before;
-        if (mine) {
+        r = p.r;
+        if (mine && p.last - p.first > 1) {
             for (; at < p.last; ++at) {
-                const Request r = request(a, at);
+                r = request(a, at);
                 const int64_t n = (int64_t)tiles_of<ROWS>(a, r, small_rows) * Hkv;
                 if (range < u + n * units_of_tile(r)) break;
                 u += n * units_of_tile(r);
@@ -156,16 +159,18 @@ __global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void 
         b = __builtin_amdgcn_readfirstlane(__shfl(at, from, 64));
         base = __shfl(u, from, 64);
         item_base = __shfl(i, from, 64);
+        r.start = __builtin_amdgcn_readfirstlane(__shfl(r.start, from, 64));
+        r.q_len = __builtin_amdgcn_readfirstlane(__shfl(r.q_len, from, 64));
+        r.n = __builtin_amdgcn_readfirstlane(__shfl(r.n, from, 64));
     }
 
     for (int64_t u0 = range; u0 < range_end;) {
-        const Request r = request(a, b);
         const int tiles = tiles_of<ROWS>(a, r, small_rows);
         const int64_t per = units_of_tile(r), whole = per * tiles * Hkv;
         if (u0 >= base + whole) {                  // (requests without queries, or with many, have no units)
             base += whole;
             item_base += (int64_t)tiles * Hkv;
-            ++b;
+            r = request(a, ++b);
             continue;
         }
         const int64_t item = divided(u0 - base, per), from_unit = u0 - base - item * per, take = min(range_end - u0, per - from_unit);
@@ -221,26 +226,31 @@ __global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void 
                 }
             }
         };
-        const bool prefix = a.n_prefix > 0 && from_unit == 0;
-        const int early = prefix ? kDepth - 2 : kDepth;    // (the prefix tokens' values take the other two places)
-        for (int i = 0; i < min(count, early); ++i) fetch(i);
-
         // ---- queries: channels as the keys' operands have them
-        v8h q[CB][NG * KS];
-        float c0[CB][NG];
+        v4u raw[CB][NG * KS];
         int limit[CB];                             // tokens that the lane's query sees
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             const int row = min(tile * ROWS + 16 * c + col, rows - 1), token = row / per_kv, q_head = head * per_kv + row % per_kv;
             limit[c] = a.causal ? max(r.n - (r.q_len - 1 - token), 0) : r.n;
             const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
+#pragma unroll
+            for (int i = 0; i < NG * KS; ++i) raw[c][i] = *reinterpret_cast<const v4u*>(src + i / KS * G + quarter * (G / 4) + 8 * (i % KS));
+        }
+        const bool prefix = a.n_prefix > 0 && from_unit == 0;
+        const int early = prefix ? kDepth - 2 : kDepth;    // (the prefix tokens' values take the other two places)
+        for (int i = 0; i < min(count, early); ++i) fetch(i);
+        v8h q[CB][NG * KS];
+        float c0[CB][NG];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
             const v4u minus8 = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 v4f z = {0, 0, 0, 0};
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    q[c][g * KS + s] = in_key_order(*reinterpret_cast<const v4u*>(src + g * G + quarter * (G / 4) + 8 * s));
+                    q[c][g * KS + s] = in_key_order(raw[c][g * KS + s]);
                     z = product(__builtin_bit_cast(v8h, minus8), q[c][g * KS + s], z);
                 }
                 c0[c][g] = z[0];
@@ -572,7 +582,7 @@ __global__ __launch_bounds__(kThreads, (Shape<D, G, DYNAMIC, CB>::PER_CU)) void 
 template <int D, int CB>
 __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items)
 {
-    constexpr int ROWS = 16 * CB, kEach = D / 64, kAtOnce = 8;
+    constexpr int ROWS = 16 * CB, kEach = D / 64;
     const int lane = threadIdx.x & 63, row = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int count = items[0].parts;
     const Item item = items[1 + blockIdx.x];                             // (of the last call, or nothing, from the count on)
@@ -597,22 +607,27 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
         sum = fmaf(sum, old, part);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) acc[i] *= old;
-        for (int i0 = 0; i0 < n; i0 += kAtOnce) {
-            float x[kAtOnce][kEach];
+        // loads of up to 32 parts at once: one after another they would take a microsecond each
+        auto add = [&](int i0, auto COUNT) PQ_INLINE {
+            constexpr int kCount = decltype(COUNT)::value;
+            float x[kCount][kEach];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < kCount; ++i) {
                 const int at = n0 + min(i0 + i, n - 1);
                 const float* src = first + at * step + (at == 0 ? second : 0) + 4 + kEach * lane;
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) x[i][k] = src[k];
             }
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < kCount; ++i) {
                 const float fi = __shfl(f, min(i0 + i, n - 1), 64);
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) acc[k] = fmaf(x[i][k], i0 + i < n ? fi : 0.0f, acc[k]);
             }
-        }
+        };
+        int i0 = 0;
+        for (; n - i0 > 8; i0 += 32) add(i0, std::integral_constant<int, 32>{});
+        if (i0 < n) add(i0, std::integral_constant<int, 8>{});
         top = to;
     }
     const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -630,13 +645,13 @@ Most at_most(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int64_t 
 {
     const int64_t by_rows = T * (n_heads / n_kv_heads) / 16 + B, by_requests = ((int64_t)small_rows + 15) / 16 * B;
     const int64_t items = (by_rows < by_requests ? by_rows : by_requests) * n_kv_heads, units = items * ((capacity + kTile - 1) / kTile);
-    return {items, (units + kLeastUnits * kWaves - 1) / (kLeastUnits * kWaves)};
+    return {items, (units + kWaves - 1) / kWaves};
 }
 
 // Scratch memory: partial sums, two to a wavefront, then the list of histories.
 size_t partial_bytes(int64_t groups, int32_t head_dim, int blocks)
 {
-    return (size_t)(groups < 768 ? groups : 768) * kWaves * 2 * 16 * blocks * (head_dim + 4) * sizeof(float);
+    return (size_t)(groups < kGroups ? groups : kGroups) * kWaves * 2 * 16 * blocks * (head_dim + 4) * sizeof(float);
 }
 
 template <int D, int G, bool DYNAMIC, int CB>
@@ -647,7 +662,7 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
     const auto kernel = k_kv4_attention_rows<D, G, DYNAMIC, CB>;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, allowed); rc != PQ_OK) return rc;
     const Most most = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page, small_rows);
-    const int64_t groups = most.groups < Shape<D, G, DYNAMIC, CB>::GROUPS ? most.groups : Shape<D, G, DYNAMIC, CB>::GROUPS;
+    const int64_t groups = most.groups < kGroups ? most.groups : kGroups;
     float* const partial = static_cast<float*>(ws);
     Item* const items = reinterpret_cast<Item*>(static_cast<uint8_t*>(ws) + partial_bytes(most.groups, D, CB));
     kernel<<<(unsigned)groups, kThreads, lds, st>>>(a, partial, items, most.items, small_rows);
