@@ -114,11 +114,11 @@ class _Declines:
     def linear(*args):
         return -1
 
-    linear2 = linear
+    linear2 = kv4_slots = kv4_append = kv4_attention = linear
 
 
 _lib = None
-_call = _Declines     # the native call path of pq_linear and pq_linear2 (csrc/pq_call.cpp)
+_call = _Declines     # the native call path of the smallest calls (csrc/pq_call.cpp)
 
 
 class PQError(RuntimeError):
@@ -137,6 +137,7 @@ def _load_call(L):
         warnings.warn("the native call path is not there (python -m paper_2410_05265_amd.build makes it); calls go through ctypes: %s" % e)
         return _Declines
     call.bind(*(ctypes.cast(getattr(L, f), _vp).value for f in ("pq_linear", "pq_linear2")))
+    call.bind_kv4(*(ctypes.cast(getattr(L, f), _vp).value for f in ("pq_kv4_slots", "pq_kv4_append", "pq_kv4_attention")))
     return call
 
 
@@ -186,6 +187,13 @@ def _check(rc: int, where: str):
 def _dev(t: torch.Tensor, dtype, what: str):
     if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise TypeError("%s must be a contiguous %s tensor on the GPU" % (what, dtype))
+
+
+def _here(t: torch.Tensor, dtype, what: str):
+    """A tensor whose kernels go to the current device's stream: it has to lie there."""
+    _dev(t, dtype, what)
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must lie on the current device" % what)
 
 
 def _reachable(t: torch.Tensor, what: str):
@@ -687,6 +695,15 @@ def pq_kv4_slots(kv_len, q_len, block_table, free_pages, page_size: int, T: int,
     """Places for a step's new tokens: kv_len, q_len int32 [B], block_table int32 [B, pages] (new entries are written), free_pages int32,
     taken int32 (pages of the list already given out; None = 0), T rows.
     Returns (cu_q int32 [B + 1], kv_len_out int32 [B], positions int32 [T], slots int64 [T], taken_out int32 [1])."""
+    if cu_q is not None and kv_len_out is not None and positions is not None and slots is not None and taken_out is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_slots(kv_len, q_len, block_table, free_pages, page_size, T, taken, position_offset, cu_q, kv_len_out, positions, slots,
+                             taken_out)
+        if rc == PQ_OK:
+            return cu_q, kv_len_out, positions, slots, taken_out
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_slots")
     device = kv_len.device
     B = kv_len.numel()
     if cu_q is None:
@@ -701,10 +718,10 @@ def pq_kv4_slots(kv_len, q_len, block_table, free_pages, page_size: int, T: int,
         taken_out = torch.empty((1,), dtype=torch.int32, device=device)
     for t, what in ((kv_len, "kv_len"), (q_len, "q_len"), (block_table, "block_table"), (free_pages, "free_pages"), (cu_q, "cu_q"),
                     (kv_len_out, "kv_len_out"), (positions, "positions"), (taken_out, "taken_out")):
-        _dev(t, torch.int32, what)
-    _dev(slots, torch.int64, "slots")
+        _here(t, torch.int32, what)
+    _here(slots, torch.int64, "slots")
     if taken is not None:
-        _dev(taken, torch.int32, "taken")
+        _here(taken, torch.int32, "taken")
     if (q_len.numel() != B or block_table.dim() != 2 or block_table.shape[0] != B or cu_q.numel() < B + 1 or kv_len_out.numel() < B or
             positions.numel() < T or slots.numel() < T or taken_out.numel() < 1 or (taken is not None and taken.numel() < 1)):
         raise ValueError("shape mismatch")
@@ -716,10 +733,10 @@ def pq_kv4_slots(kv_len, q_len, block_table, free_pages, page_size: int, T: int,
 
 def _kv4_cache(k_codes, v_codes, k_scale, v_scale, group: int):
     """The cache of one layer as the library takes it; sizes from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
-    _dev(k_codes, torch.uint8, "k_codes")
-    _dev(v_codes, torch.uint8, "v_codes")
-    _dev(k_scale, torch.float32, "k_scale")
-    _dev(v_scale, torch.float32, "v_scale")
+    _here(k_codes, torch.uint8, "k_codes")
+    _here(v_codes, torch.uint8, "v_codes")
+    _here(k_scale, torch.float32, "k_scale")
+    _here(v_scale, torch.float32, "v_scale")
     if k_codes.dim() != 4 or v_codes.shape != k_codes.shape:
         raise ValueError("shape mismatch")
     n_pages, heads, page_size, half = k_codes.shape
@@ -733,33 +750,45 @@ def _rows(t: torch.Tensor, what: str):
     """A matrix of fp16 rows, which may lie apart."""
     if not t.is_cuda or t.dtype != torch.float16 or t.dim() != 2 or t.stride(1) != 1:
         raise TypeError("%s must be a %s matrix with contiguous rows on the GPU" % (what, torch.float16))
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must lie on the current device" % what)
 
 
 def pq_kv4_append(qkv, n_heads: int, positions, slots, k_codes, v_codes, k_scale, v_scale, q_weight=None, k_weight=None, eps: float = 1e-6,
                   cos_sin=None, interleaved: bool = False, rotate: bool = True, group: int = 0, clip: float = 1.0, out=None):
     """qkv fp16 [T, (n_heads + 2 kv heads) * head_dim] -> turned queries fp16 [T, n_heads * head_dim]; the codes of keys and values go to
     their slots (int64 [T]) of the cache, with group > 0 their steps too.  cos_sin: fp32 [positions, rotary_dim] or None."""
+    if out is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_append(qkv, n_heads, positions, slots, k_codes, v_codes, k_scale, v_scale, q_weight, k_weight, eps, cos_sin, interleaved,
+                              rotate, group, clip, out)
+        if rc == PQ_OK:
+            return out
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_append")
     cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
     _rows(qkv, "qkv")
-    _dev(slots, torch.int64, "slots")
+    _here(slots, torch.int64, "slots")
     T, D = qkv.shape[0], cache.head_dim
     if qkv.shape[1] != (n_heads + 2 * cache.n_kv_heads) * D or slots.numel() != T:
         raise ValueError("shape mismatch")
     for w in (q_weight, k_weight):
         if w is not None:
-            _dev(w, torch.float16, "weight")
+            _here(w, torch.float16, "weight")
             if w.numel() != D:
                 raise ValueError("shape mismatch")
     rd = 0
     if cos_sin is not None:
-        _dev(cos_sin, torch.float32, "cos_sin")
-        _dev(positions, torch.int32, "positions")
+        _here(cos_sin, torch.float32, "cos_sin")
+        _here(positions, torch.int32, "positions")
         if cos_sin.dim() != 2 or positions.numel() != T:
             raise ValueError("shape mismatch")
         rd = cos_sin.shape[1]
     if out is None:
         out = torch.empty((T, n_heads * D), dtype=torch.float16, device=qkv.device)
     else:
+        _here(out, torch.float16, "out")
         _result(out, T * n_heads * D, "out")
     _check(lib().pq_kv4_append(_ptr(qkv), qkv.stride(0) if T > 1 else qkv.shape[1], T, int(n_heads), _ptr(positions), _ptr(slots), _ptr(q_weight),
                                _ptr(k_weight), float(eps), _ptr(cos_sin), 0 if cos_sin is None else cos_sin.shape[0], rd, int(bool(interleaved)),
@@ -778,11 +807,20 @@ def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_
                      prefix_k=None, prefix_v=None, causal: bool = True, out=None, workspace=None):
     """Attention of q fp16 [T, n_heads * head_dim] over the cache behind optional prefix tokens (fp16 [n, kv heads, head_dim]): rows
     cu_q[b] .. cu_q[b + 1] are request b's, whose kv_len[b] tokens lie in the pages block_table[b].  Returns (out, workspace)."""
+    if out is not None and workspace is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k, prefix_v,
+                                 causal, out, workspace)
+        if rc == PQ_OK:
+            return out, workspace
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_attention")
     cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
     _rows(q, "q")
-    _dev(cu_q, torch.int32, "cu_q")
-    _dev(kv_len, torch.int32, "kv_len")
-    _dev(block_table, torch.int32, "block_table")
+    _here(cu_q, torch.int32, "cu_q")
+    _here(kv_len, torch.int32, "kv_len")
+    _here(block_table, torch.int32, "block_table")
     T, D, B = q.shape[0], cache.head_dim, kv_len.numel()
     n_heads = q.shape[1] // D
     n_prefix = 0 if prefix_k is None else prefix_k.shape[0]
@@ -792,7 +830,7 @@ def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_
         raise ValueError("prefix_k and prefix_v come together")
     if n_prefix:
         for t, what in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
-            _dev(t, torch.float16, what)
+            _here(t, torch.float16, what)
             if tuple(t.shape) != (n_prefix, cache.n_kv_heads, D):
                 raise ValueError("shape mismatch")
     W = block_table.shape[1]
@@ -800,10 +838,11 @@ def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_
         need = int(lib().pq_kv4_attention_workspace_bytes(T, B, n_heads, int(max_q), W, cache))
         workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=q.device)
     else:
-        _dev(workspace, torch.uint8, "workspace")
+        _here(workspace, torch.uint8, "workspace")
     if out is None:
         out = torch.zeros((T, n_heads * D), dtype=torch.float16, device=q.device)
     else:
+        _here(out, torch.float16, "out")
         _result(out, T * n_heads * D, "out")
     _check(lib().pq_kv4_attention(_ptr(q), q.stride(0) if T > 1 else q.shape[1], T, n_heads, _ptr(cu_q), _ptr(kv_len), B, int(max_q),
                                   _ptr(block_table), W, cache, _ptr(prefix_k), _ptr(prefix_v), n_prefix, float(softmax_scale), int(bool(causal)),
