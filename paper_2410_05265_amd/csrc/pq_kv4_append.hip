@@ -43,13 +43,24 @@ struct Lane {
     float x[8];
     float w[8];           // the norm's weight, or 1
     float cs[8], sn[8];   // cosine and sine of each channel's angle, the sine with the sign it enters with; 1 and 0 where nothing turns
-    int partner;          // lane whose channels turn with this one's (halves), or -1: neighbouring channels turn
+    int partner;          // lane whose channels turn with this one's (halves of less than a head)
 };
 
+// Which channels turn together: none; neighbours; those half a head apart, in lanes one bit apart; those half of rotary_dim apart.
+enum Turn { kNone, kPairs, kHalfHead, kHalves };
+
+template <int LOG2_D> __device__ __forceinline__ constexpr double inv_sqrt()       // 1 / sqrt(D)
+{
+    static_assert(LOG2_D == 6 || LOG2_D == 7, "heads of 64 or 128 channels");
+    return LOG2_D == 6 ? 0.125 : 0.08838834764831845;
+}
+
+// In fp32 the Hadamard rotation's values carry the sign of rq::lane_sign, which whoever takes them multiplies in.
 template <typename F, int LOG2_D, bool ROTATE>
-__device__ __forceinline__ void turn(const Lane& c, bool norm, bool rope, F eps, int lane, F (&v)[8])
+__device__ __forceinline__ void turn(const Lane& c, bool norm, Turn rope, F eps, int lane, F (&v)[8])
 {
     constexpr int kLaneBits = LOG2_D - 3;
+    constexpr bool kExact = std::is_same<F, double>::value;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (F)c.x[i];
     if (norm) {
@@ -59,14 +70,17 @@ __device__ __forceinline__ void turn(const Lane& c, bool norm, bool rope, F eps,
         sum = sum_lanes<kLaneBits>(sum);
         const F mean = sum * (F)(1.0 / (1 << LOG2_D)) + eps;
         F scale;
-        if constexpr (std::is_same<F, double>::value) scale = 1.0 / sqrt(mean);
+        if constexpr (kExact) scale = 1.0 / sqrt(mean);
         else scale = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= scale * (F)c.w[i];
     }
-    if (rope) {
+    if (rope != kNone) {
         F other[8];
-        if (c.partner >= 0) {
+        if (rope == kHalfHead) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = from_lane_xor<kLaneBits - 1>(v[i]);
+        } else if (rope == kHalves) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) other[i] = __shfl(v[i], c.partner, 64);
         } else {
@@ -77,12 +91,9 @@ __device__ __forceinline__ void turn(const Lane& c, bool norm, bool rope, F eps,
         for (int i = 0; i < 8; ++i) v[i] = v[i] * (F)c.cs[i] + other[i] * (F)c.sn[i];
     }
     if constexpr (ROTATE) {
-        if constexpr (std::is_same<F, float>::value) {
+        if constexpr (!kExact) {
             rq::reg_stages8(v, 3);
             static_for<0, kLaneBits>([&](auto B) { rq::lane_stage<decltype(B)::value>(v, lane); });
-            const float sign = rq::lane_sign(lane, kLaneBits);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= sign;
         } else {
             static_for<0, 3>([&](auto S) {
                 constexpr int d = 1 << decltype(S)::value;
@@ -128,42 +139,165 @@ __device__ __forceinline__ uint32_t codes8(const double (&t)[8])
     return s;
 }
 
+__device__ __forceinline__ void halves_to_floats(const v4i raw, float (&v)[8])
+{
+    const __half2* h = reinterpret_cast<const __half2*>(&raw);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(h[i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+
+// Stores the codes of a wavefront's vectors, and the steps where they are dynamic.
+template <int LOG2_D, int LOG2_GROUP>
+__device__ __forceinline__ void store_codes(const AppendArgs& a, bool is_value, int64_t token, int c, uint32_t codes, float step)
+{
+    constexpr int D = 1 << LOG2_D, kGroupBits = LOG2_GROUP ? LOG2_GROUP - 3 : LOG2_D - 3;
+    reinterpret_cast<uint32_t*>((is_value ? a.cache.v_codes : a.cache.k_codes) + token * (D / 2))[c] = codes;
+    if constexpr (LOG2_GROUP != 0) {
+        if ((c & ((1 << kGroupBits) - 1)) == 0) (is_value ? a.cache.v_scale : a.cache.k_scale)[token * (D >> LOG2_GROUP) + (c >> kGroupBits)] = step;
+    }
+}
+
+// Codes (and steps) of key or value vectors by the definition in fp64, for those vectors of the wavefront that `wanted` has a lane of.
 template <int LOG2_D, int LOG2_GROUP, bool ROTATE>
+__device__ __forceinline__ void append_exact(const AppendArgs& a, Lane& ln, Turn rope, int head, int64_t token0, uint64_t wanted, int lane)
+{
+    constexpr int kLanes = (1 << LOG2_D) / 8, kLaneBits = LOG2_D - 3;
+    constexpr int kGroupBits = LOG2_GROUP ? LOG2_GROUP - 3 : kLaneBits;
+    const int c = lane & (kLanes - 1), Hkv = a.cache.n_kv_heads;
+    const bool is_value = head >= a.n_heads + Hkv;
+    const int kv_head = head - a.n_heads - (is_value ? Hkv : 0);
+    double d[8];
+    if (is_value) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = (double)ln.x[i];
+    } else {
+        if (a.k_weight) halves_to_floats(*reinterpret_cast<const v4i*>(a.k_weight + 8 * c), ln.w);
+        turn<double, LOG2_D, ROTATE>(ln, a.k_weight != nullptr, rope, (double)a.eps, lane, d);
+        if constexpr (ROTATE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] *= inv_sqrt<LOG2_D>();
+        }
+    }
+    float step;
+    if constexpr (LOG2_GROUP == 0) {
+        step = (is_value ? a.cache.v_scale : a.cache.k_scale)[kv_head];
+    } else {
+        double most = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmax(most, fabs(d[i]));
+        step = (float)((double)a.clip * max_lanes<kGroupBits>(most) / 7.0);
+        if (!(step > 0.0f)) step = 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] /= (double)step;
+    if ((wanted >> (lane & ~(kLanes - 1))) & ((1ull << kLanes) - 1))
+        store_codes<LOG2_D, LOG2_GROUP>(a, is_value, token0 + ((int64_t)kv_head << a.cache.log2_page), c, codes8(d), step);
+}
+
+// The head vectors of one head of the wavefront's tokens: a query's channels, or the codes of a key or value.  Returns the lanes whose
+// codes the fp32 path cannot decide; their vectors are left to append_exact.
+template <int LOG2_D, int LOG2_GROUP, bool ROTATE>
+__device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, Turn rope, const v4i raw, int head, __half* q_row, int64_t token0, bool live, int lane)
+{
+    constexpr int D = 1 << LOG2_D, kLanes = D / 8, kLaneBits = LOG2_D - 3;
+    constexpr int kGroupBits = LOG2_GROUP ? LOG2_GROUP - 3 : kLaneBits;
+    const int c = lane & (kLanes - 1), Hkv = a.cache.n_kv_heads;
+    const bool is_query = head < a.n_heads, is_value = head >= a.n_heads + Hkv;
+    const bool norm = !is_value && (is_query ? a.q_weight : a.k_weight) != nullptr;
+    if (norm) halves_to_floats(*reinterpret_cast<const v4i*>((is_query ? a.q_weight : a.k_weight) + 8 * c), ln.w);
+    halves_to_floats(raw, ln.x);
+    const double unit = ROTATE && !is_value ? inv_sqrt<LOG2_D>() : 1.0;
+    const float sign = ROTATE && !is_value ? rq::lane_sign(lane, kLaneBits) : 1.0f;
+
+    float v[8];
+    if (is_value) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = ln.x[i];
+    } else {
+        turn<float, LOG2_D, ROTATE>(ln, norm, rope, a.eps, lane, v);
+    }
+    if (is_query) {
+        const float m = (float)unit * sign;
+        v4i o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 h = __floats2half2_rn(v[2 * i] * m, v[2 * i + 1] * m);
+            o[i] = *reinterpret_cast<const int*>(&h);
+        }
+        if (live) *reinterpret_cast<v4i*>(q_row + head * D) = o;
+        return 0;
+    }
+
+    const int kv_head = head - a.n_heads - (is_value ? Hkv : 0);
+    const int64_t token = token0 + ((int64_t)kv_head << a.cache.log2_page);       // of this head in the cache
+    float* const scales = is_value ? a.cache.v_scale : a.cache.k_scale;
+    float step;
+    if constexpr (LOG2_GROUP == 0) {
+        step = scales[kv_head];
+    } else {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
+        step = (float)((double)a.clip * ((double)max_lanes<kGroupBits>(most) * unit) / 7.0);
+        if (!(step > 0.0f)) step = 1.0f;
+    }
+    const float mult = (float)unit / step * sign;
+    float t8[8], norm2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        t8[i] = v[i] * mult;
+        norm2 = fmaf(t8[i], t8[i], norm2);
+    }
+    // The multiplier and its product are off by 2^-22 of a quotient, 2^-19 at the end of the range.  Norm, position rotation and
+    // butterflies are orthogonal up to a factor: each rounds by 2^-24 of the vector's length at most and passes on what came before, 12 such
+    // roundings in all, and the norm's factor itself is within 2^-21 of its value, 2^-18 at the end of the range.
+    float near = 0x1.0p-17f;
+    if (!is_value) near += 0x1.0p-20f * __builtin_amdgcn_sqrtf(sum_lanes<kLaneBits>(norm2));
+    bool suspect;
+    const uint32_t codes = codes8(t8, near, suspect);
+    const uint64_t found = __builtin_amdgcn_ballot_w64(suspect && live);
+    // (by vector: what a token gets does not depend on its neighbours)
+    if (live && ((found >> (lane & ~(kLanes - 1))) & ((1ull << kLanes) - 1)) == 0) store_codes<LOG2_D, LOG2_GROUP>(a, is_value, token, c, codes, step);
+    return found;
+}
+
+// One head to a wavefront, or (MANY) eight, every fourth one: then what belongs to the token (its place, its angles) is read once for
+// them, the next head's values are on their way while one is turned, and the vectors for the fp64 path wait to the end, so that their
+// registers are not held in the loop.
+constexpr int kMany = 8;
+template <int LOG2_D, int LOG2_GROUP, bool ROTATE, bool MANY>
 __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
 {
-    constexpr int D = 1 << LOG2_D, kLanes = D / 8, kTokens = 64 / kLanes, kLaneBits = LOG2_D - 3;
-    constexpr int kGroupBits = LOG2_GROUP ? LOG2_GROUP - 3 : kLaneBits;
-    const int lane = threadIdx.x & 63, c = lane & (kLanes - 1);
-    const int head = blockIdx.y * (kThreads / 64) + (threadIdx.x >> 6);
-    const int Hkv = a.cache.n_kv_heads;
-    if (head >= a.n_heads + 2 * Hkv) return;                             // whole wavefronts; nothing synchronises the workgroup
+    constexpr int D = 1 << LOG2_D, kLanes = D / 8, kTokens = 64 / kLanes, kStride = kThreads / 64;
+    const int lane = threadIdx.x & 63, c = lane & (kLanes - 1), heads = a.n_heads + 2 * a.cache.n_kv_heads;
+    constexpr int each = MANY ? kMany : 1;
+    int head = blockIdx.y * (kStride * each) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (head >= heads) return;                                           // whole wavefronts; nothing synchronises the workgroup
     const int64_t t = (int64_t)blockIdx.x * kTokens + lane / kLanes, row = min(t, a.T - 1);
+    const __half* src = a.qkv + row * a.row_stride + 8 * c;
+    auto load = [&](int h) { return __builtin_nontemporal_load(reinterpret_cast<const v4i*>(src + (int64_t)h * D)); };
+    v4i raw = load(head);
     const int64_t slot = a.slots[row];
     const bool live = t < a.T && slot >= 0 && slot < a.cache.n_pages << a.cache.log2_page;
     if (__builtin_amdgcn_ballot_w64(live) == 0) return;
-    const bool is_query = head < a.n_heads, is_value = head >= a.n_heads + Hkv;
+    __half* const q_row = a.q_out + row * a.n_heads * D + 8 * c;
+    // head 0's place in the cache; a head further on lies a page further
+    const int64_t token0 = (((slot >> a.cache.log2_page) * a.cache.n_kv_heads) << a.cache.log2_page) + (slot & ((1ll << a.cache.log2_page) - 1));
 
     Lane ln;
-    const v4i raw = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(a.qkv + row * a.row_stride + (int64_t)head * D + 8 * c));
-    const bool norm = !is_value && (is_query ? a.q_weight : a.k_weight) != nullptr;
-    const bool rope = !is_value && a.cos_sin != nullptr;
-    if (norm) {
-        const v4i w = *reinterpret_cast<const v4i*>((is_query ? a.q_weight : a.k_weight) + 8 * c);
-        const __half2* h = reinterpret_cast<const __half2*>(&w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = __half22float2(h[i]);
-            ln.w[2 * i] = f.x;
-            ln.w[2 * i + 1] = f.y;
-        }
-    }
-    ln.partner = -1;
-    if (rope) {
+    Turn rope = kNone;
+    if (a.cos_sin != nullptr && head < a.n_heads + a.cache.n_kv_heads) {
         const int half = a.rotary_dim / 2;
         const int64_t position = min(max((int64_t)a.positions[row], (int64_t)0), a.max_positions - 1);
         const float* cs = a.cos_sin + position * a.rotary_dim;
         const bool turns = 8 * c < a.rotary_dim;
+        ln.partner = lane;
         if (a.interleaved) {
+            rope = kPairs;
             const float4 x = *reinterpret_cast<const float4*>(cs + (turns ? 4 * c : 0)), y = *reinterpret_cast<const float4*>(cs + half + (turns ? 4 * c : 0));
             const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -173,9 +307,10 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
                 ln.sn[2 * i + 1] = turns ? ys[i] : 0.0f;
             }
         } else {
+            rope = a.rotary_dim == D ? kHalfHead : kHalves;
             const bool first = 8 * c < half;
             const int at = turns ? (first ? 8 * c : 8 * c - half) : 0;
-            ln.partner = turns ? (first ? lane + half / 8 : lane - half / 8) : lane;
+            if (turns) ln.partner = first ? lane + half / 8 : lane - half / 8;
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {
                 const float4 x = *reinterpret_cast<const float4*>(cs + at + i), y = *reinterpret_cast<const float4*>(cs + half + at + i);
@@ -188,109 +323,61 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
             }
         }
     }
-    {
-        const __half2* h = reinterpret_cast<const __half2*>(&raw);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = __half22float2(h[i]);
-            ln.x[2 * i] = f.x;
-            ln.x[2 * i + 1] = f.y;
-        }
-    }
-    constexpr double kInvSqrt = LOG2_D == 6 ? 0.125 : 0.08838834764831845;   // 1 / sqrt(D)
-    static_assert(LOG2_D == 6 || LOG2_D == 7, "heads of 64 or 128 channels");
-    const double unit = ROTATE && !is_value ? kInvSqrt : 1.0;
-
-    float v[8];
-    if (is_value) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = ln.x[i];
-    } else {
-        turn<float, LOG2_D, ROTATE>(ln, norm, rope, a.eps, lane, v);
-    }
-    if (is_query) {
-        const float m = (float)unit;
-        v4i o;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __half2 h = __floats2half2_rn(v[2 * i] * m, v[2 * i + 1] * m);
-            o[i] = *reinterpret_cast<const int*>(&h);
-        }
-        if (live) *reinterpret_cast<v4i*>(a.q_out + (t * a.n_heads + head) * D + 8 * c) = o;
+    if constexpr (!MANY) {
+        const uint64_t found = append_head<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, raw, head, q_row, token0, live, lane);
+        if (found != 0) append_exact<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, head, token0, found, lane);
         return;
     }
+    __shared__ uint64_t suspects[kStride][kMany];                   // of each wavefront's own
+    const int first_head = head, wave = threadIdx.x >> 6, end = min(heads, head + kStride * each);
+    uint32_t asked = 0;
+#pragma unroll 1
+    for (int j = 0;; ++j) {
+        const v4i now = raw;
+        if (head + kStride < end) raw = load(head + kStride);
+        const uint64_t found = append_head<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, now, head, q_row, token0, live, lane);
+        if (found != 0) {
+            asked |= 1u << j;
+            suspects[wave][j] = found;
+        }
+        head += kStride;
+        if (head >= end) break;
+    }
+#pragma unroll 1
+    for (; asked != 0; asked &= asked - 1) {
+        const int j = __builtin_ctz(asked);
+        const int again = first_head + j * kStride;
+        halves_to_floats(load(again), ln.x);
+        // (what derives from these is computed here, and not once in front of the loop, where it would hold twice their registers)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(ln.cs[i]), "+v"(ln.sn[i]));
+        append_exact<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, again, token0, suspects[wave][j], lane);
+    }
+}
 
-    const int kv_head = head - a.n_heads - (is_value ? Hkv : 0);
-    const int64_t page = slot >> a.cache.log2_page, at = slot & ((1ll << a.cache.log2_page) - 1);
-    const int64_t token = (((page * Hkv + kv_head) << a.cache.log2_page) + at);   // of this head in the cache
-    float* const scales = is_value ? a.cache.v_scale : a.cache.k_scale;
-    float step;
-    if constexpr (LOG2_GROUP == 0) {
-        step = scales[kv_head];
-    } else {
-        float most = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
-        step = (float)((double)a.clip * ((double)max_lanes<kGroupBits>(most) * unit) / 7.0);
-        if (!(step > 0.0f)) step = 1.0f;
-    }
-    const float mult = (float)(unit / (double)step);
-    float t8[8], norm2 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        t8[i] = v[i] * mult;
-        norm2 = fmaf(t8[i], t8[i], norm2);
-    }
-    // The reciprocal and its product are off by 2^-23 of a quotient, 2^-20 at the end of the range.  Norm, position rotation and
-    // butterflies are orthogonal up to a factor: each rounds by 2^-24 of the vector's length at most and passes on what came before, 12 such
-    // roundings in all, and the norm's factor itself is within 2^-21 of its value, 2^-18 at the end of the range.
-    float near = 0x1.0p-17f;
-    if (!is_value) near += 0x1.0p-20f * __builtin_amdgcn_sqrtf(sum_lanes<kLaneBits>(norm2));
-    bool suspect;
-    uint32_t codes = codes8(t8, near, suspect);
-    if (const uint64_t found = __builtin_amdgcn_ballot_w64(suspect && live); found != 0) {
-        double d[8];
-        if (is_value) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = (double)ln.x[i];
-        } else {
-            turn<double, LOG2_D, ROTATE>(ln, norm, rope, (double)a.eps, lane, d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] *= unit;
-        }
-        float exact_step = step;
-        if constexpr (LOG2_GROUP != 0) {
-            double most = 0.0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) most = fmax(most, fabs(d[i]));
-            exact_step = (float)((double)a.clip * max_lanes<kGroupBits>(most) / 7.0);
-            if (!(exact_step > 0.0f)) exact_step = 1.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] /= (double)exact_step;
-        const uint32_t exact = codes8(d);
-        // only the vectors that asked for it: what a token gets does not depend on its neighbours
-        if ((found >> (lane & ~(kLanes - 1))) & ((1ull << kLanes) - 1)) {
-            codes = exact;
-            step = exact_step;
-        }
-    }
-    if (!live) return;
-    reinterpret_cast<uint32_t*>((is_value ? a.cache.v_codes : a.cache.k_codes) + token * (D / 2))[c] = codes;
-    if constexpr (LOG2_GROUP != 0) {
-        if ((c & ((1 << kGroupBits) - 1)) == 0) scales[token * (D >> LOG2_GROUP) + (c >> kGroupBits)] = step;
-    }
+template <int LOG2_D, int LOG2_GROUP, bool ROTATE>
+int launch(const AppendArgs& a, hipStream_t st)
+{
+    constexpr int kTokens = 64 / ((1 << LOG2_D) / 8);
+    const int64_t blocks = (a.T + kTokens - 1) / kTokens;
+    const int heads = a.n_heads + 2 * a.cache.n_kv_heads;
+    // Eight heads to a wavefront once one to each would be more than about two wavefronts to every place on the card (5 to 8 a SIMD, 1024
+    // SIMDs).  48 heads of 128, one | eight: 512 tokens (6144 wavefronts) 8.3 | 8.2 us, 1000 12.4 | 11.7, 2000 20.0 | 16.4, 8192 62 | 47,
+    // 16000 116 | 86; 80 heads with dynamic steps and norms: 512 tokens (10240) 11.8 | 13.1, 1000 18.8 | 17.7, 8000 107 | 86; 48 heads of
+    // 64: 512 tokens 6.3 | 7.7, 2000 (12000) 12.2 | 12.5, 8000 31.7 | 27.2.  With twelve a step of 64 tokens takes twice as long, with
+    // four 8192 tokens 50.
+    const bool many = blocks * heads > 12288;
+    const int each = 4 * (many ? kMany : 1);                             // heads of a workgroup
+    const dim3 grid((unsigned)blocks, (unsigned)((heads + each - 1) / each));
+    if (many) k_kv4_append<LOG2_D, LOG2_GROUP, ROTATE, true><<<grid, kThreads, 0, st>>>(a);
+    else k_kv4_append<LOG2_D, LOG2_GROUP, ROTATE, false><<<grid, kThreads, 0, st>>>(a);
+    return hip_status(hipGetLastError());
 }
 
 template <int LOG2_D, int LOG2_GROUP>
 int launch(const AppendArgs& a, bool rotate, hipStream_t st)
 {
-    constexpr int kTokens = 64 / ((1 << LOG2_D) / 8);
-    const int64_t blocks = (a.T + kTokens - 1) / kTokens;
-    const dim3 grid((unsigned)blocks, (unsigned)((a.n_heads + 2 * a.cache.n_kv_heads + 3) / 4));
-    if (rotate) k_kv4_append<LOG2_D, LOG2_GROUP, true><<<grid, kThreads, 0, st>>>(a);
-    else k_kv4_append<LOG2_D, LOG2_GROUP, false><<<grid, kThreads, 0, st>>>(a);
-    return hip_status(hipGetLastError());
+    return rotate ? launch<LOG2_D, LOG2_GROUP, true>(a, st) : launch<LOG2_D, LOG2_GROUP, false>(a, st);
 }
 
 }  // namespace
