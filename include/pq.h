@@ -559,8 +559,8 @@ typedef struct pq_kv4_cache {
  *     taken_out[0] = taken + sum of need_b: above n_free if the list was too short.
  * Rows behind the last request up to T (a padded step) get position 0 and slot -1; tokens past row T are not written.  position_offset:
  * the prefix tokens in front (>= 0).  taken: device int32, or NULL for 0; with taken_out of the last call the list is used on.
- * All arrays int32 and 4-byte aligned but slots (int64 [T], 8-byte aligned); positions [T].  Outputs may not lie over kv_len, q_len or taken
- * (PQ_ERR_UNSUPPORTED).  B >= 0, T >= 0 and below 2^31; table_pages >= 1; n_free >= 0.
+ * All arrays int32 and 4-byte aligned but slots (int64 [T], 8-byte aligned); positions [T].  Outputs may not lie over kv_len, q_len,
+ * free_pages or taken (PQ_ERR_UNSUPPORTED).  0 <= B < 2^26; 0 <= T < 2^31; table_pages >= 1; n_free >= 0.
  */
 int pq_kv4_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t* block_table, int32_t table_pages,
                  const int32_t* free_pages, int32_t n_free, const int32_t* taken, int32_t page_size, int64_t T, int32_t position_offset,
@@ -579,10 +579,10 @@ int pq_kv4_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t
  * q_out_f16 out [T, n_heads * head_dim] fp16: the queries' z (fp32 path, rounded once); may not lie over qkv (PQ_ERR_UNSUPPORTED).
  * Keys' z and values' x go to slots[t] (int64: page * page_size + place) of the cache as clamp(round_half_even(z / step), -8, 7): with
  *     group = 0 the head's static step, else step = fp32(clip * max |z| over the group / 7), 1 for a group of zeros, which is
- *     written as well; clip in (0, 1].  The codes are those of this definition in double precision (dynamic steps: of an fp32 step within
- *     2^-22 of it).
+ *     written as well; clip in (0, 1].  The codes are those of this definition in double precision, dynamic ones with the step that is
+ *     written: a value's is exact, a key's off by its fp32 path, 2^-20 of the head vector's length / 7 and 2^-20 of itself at most.
  * Tokens whose slot lies outside the cache (-1 of a padded step) are neither read nor written, in the cache and in q_out.  Two tokens with the
- * same slot leave the codes of either.  T * (n_heads + 2 n_kv_heads) < 2^31.
+ * same slot leave the codes of either, channel by channel.  n_heads is a multiple of n_kv_heads; T < 2^25, T * (n_heads + 2 n_kv_heads) < 2^31.
  */
 int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* positions, const int64_t* slots,
                   const void* q_weight_f16, const void* k_weight_f16, float eps, const float* cos_sin, int64_t max_positions,
@@ -603,8 +603,10 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
  * out_f16   out [T, n_heads * head_dim] fp16; rows outside [cu_q[0], cu_q[B]) are left as they were; may not lie over q.
  * Scores, sums and the softmax's statistics are fp32; the probabilities are rounded to fp16 for the second product, and the sum that divides
  * it is theirs.  Sums are taken in an order that depends on the sizes and lengths alone: results are reproducible.
- * workspace: device memory, 256-byte aligned, pq_kv4_attention_workspace_bytes of the same arguments (at most 160 MiB).
- * T * n_heads < 2^31.
+ * workspace: device memory, 256-byte aligned, pq_kv4_attention_workspace_bytes of the same arguments (at most 160 MiB, and 2 bytes for each
+ *     of T * n_heads + 16 * B * n_kv_heads; 0 for sizes that the call refuses).  What it holds need not be set, and calls that may run at
+ *     the same time (two streams, two captured graphs) need one each.
+ * n_heads is a multiple of n_kv_heads; T * n_heads and table_pages * page_size < 2^30, B * n_kv_heads < 2^21.
  */
 size_t pq_kv4_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages,
                                         const pq_kv4_cache* cache);

@@ -37,6 +37,13 @@ int check_cache(const pq_kv4_cache* c, pq::kv4::Cache* out)
     return PQ_OK;
 }
 
+// The sizes of an attention call: tokens of a request count as int32, and a launch holds at most 2^32 threads.
+bool attention_sizes_ok(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, const pq_kv4_cache* c)
+{
+    return T >= 0 && B >= 0 && n_heads >= 1 && n_heads % c->n_kv_heads == 0 && T < 1 << 30 && T * n_heads < 1 << 30 && (int64_t)B * c->n_kv_heads < 1 << 21 &&
+           max_q >= 1 && table_pages >= 1 && (int64_t)table_pages * c->page_size < 1 << 30;
+}
+
 }  // namespace
 
 extern "C" {
@@ -45,7 +52,7 @@ int pq_kv4_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t
                  const int32_t* free_pages, int32_t n_free, const int32_t* taken, int32_t page_size, int64_t T, int32_t position_offset,
                  int32_t* cu_q, int32_t* kv_len_out, int32_t* positions, int64_t* slots, int32_t* taken_out, void* stream)
 {
-    if (B < 0 || T < 0 || T > INT32_MAX || table_pages < 1 || n_free < 0 || position_offset < 0 || !page_size_ok(page_size)) return PQ_ERR_SHAPE;
+    if (B < 0 || B >= 1 << 26 || T < 0 || T > INT32_MAX || table_pages < 1 || n_free < 0 || position_offset < 0 || !page_size_ok(page_size)) return PQ_ERR_SHAPE;
     if ((B > 0 && (!kv_len || !q_len || !block_table || !kv_len_out)) || (n_free > 0 && !free_pages) || !cu_q || !taken_out ||
         (T > 0 && (!positions || !slots)))
         return PQ_ERR_NULL;
@@ -72,7 +79,7 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
     pq::kv4::Cache c;
     if (const int rc = check_cache(cache, &c); rc != PQ_OK) return rc;
     const int64_t heads = (int64_t)n_heads + 2ll * c.n_kv_heads, D = cache->head_dim;
-    if (T < 0 || n_heads < 1 || n_heads % c.n_kv_heads != 0 || heads > 65535 || T * heads > INT32_MAX) return PQ_ERR_SHAPE;
+    if (T < 0 || n_heads < 1 || n_heads % c.n_kv_heads != 0 || heads > 65535 || T >= 1 << 25 || T * heads > INT32_MAX) return PQ_ERR_SHAPE;
     if (row_stride < heads * D || row_stride % 8 != 0) return PQ_ERR_SHAPE;
     if (cos_sin && (max_positions < 1 || rotary_dim < 16 || rotary_dim > D || rotary_dim % 16 != 0)) return PQ_ERR_SHAPE;
     if (!isfinite(eps) || eps < 0.0f) return PQ_ERR_SHAPE;
@@ -91,9 +98,7 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
 
 size_t pq_kv4_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, const pq_kv4_cache* cache)
 {
-    if (check_cache_shape(cache) != PQ_OK || T <= 0 || B <= 0 || n_heads < 1 || n_heads % cache->n_kv_heads != 0 || max_q < 1 || table_pages < 1 ||
-        T > INT32_MAX / n_heads)
-        return 0;
+    if (check_cache_shape(cache) != PQ_OK || T <= 0 || B <= 0 || !attention_sizes_ok(T, B, n_heads, max_q, table_pages, cache)) return 0;
     return pq::kv4::attention_workspace_bytes(T, B, n_heads, cache->n_kv_heads, cache->head_dim, max_q, (int64_t)table_pages * cache->page_size);
 }
 
@@ -105,8 +110,7 @@ int pq_kv4_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n
     pq::kv4::Cache c;
     if (const int rc = check_cache(cache, &c); rc != PQ_OK) return rc;
     const int64_t D = cache->head_dim;
-    if (T < 0 || B < 0 || n_heads < 1 || n_heads % c.n_kv_heads != 0 || T > INT32_MAX / n_heads || max_q < 1 || table_pages < 1) return PQ_ERR_SHAPE;
-    if ((int64_t)table_pages * cache->page_size > INT32_MAX / 2 || n_prefix < 0 || n_prefix > 1024) return PQ_ERR_SHAPE;
+    if (!attention_sizes_ok(T, B, n_heads, max_q, table_pages, cache) || n_prefix < 0 || n_prefix > 1024) return PQ_ERR_SHAPE;
     if (row_stride < n_heads * D || row_stride % 8 != 0) return PQ_ERR_SHAPE;
     if (!(isfinite(softmax_scale) && softmax_scale > 0.0f)) return PQ_ERR_SCALE;
     if (T == 0 || B == 0) return PQ_OK;

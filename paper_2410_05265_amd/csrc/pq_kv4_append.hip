@@ -252,9 +252,10 @@ __device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, T
         t8[i] = v[i] * mult;
         norm2 = fmaf(t8[i], t8[i], norm2);
     }
-    // The multiplier and its product are off by 2^-22 of a quotient, 2^-19 at the end of the range.  Norm, position rotation and
-    // butterflies are orthogonal up to a factor: each rounds by 2^-24 of the vector's length at most and passes on what came before, 12 such
-    // roundings in all, and the norm's factor itself is within 2^-21 of its value, 2^-18 at the end of the range.
+    // The multiplier and its product are off by 1.5 * 2^-23 of a quotient, 1.5 * 2^-20 at the end of the range.  Norm, position rotation and
+    // butterflies are orthogonal up to a factor: each rounds by 2^-24 of the vector's length at most and passes on what came before, 11 such
+    // roundings in all, and the norm's factor itself is within 8.5 * 2^-24 of its value (half the 12 roundings of the sum of squares, half
+    // of the mean's, the reciprocal root's 2^-23), 8.5 * 2^-21 at the end of the range: with the first less than 2^-17.
     float near = 0x1.0p-17f;
     if (!is_value) near += 0x1.0p-20f * __builtin_amdgcn_sqrtf(sum_lanes<kLaneBits>(norm2));
     bool suspect;

@@ -578,15 +578,11 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
     }
 }
 
-// Adds the partial sums of the histories that were cut: a workgroup takes four rows of one, one to a wavefront.
+// Row `row` of one history that was cut, by a wavefront.
 template <int D, int CB>
-__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items)
+__device__ __forceinline__ void join(const AttentionArgs& a, const float* __restrict__ partial, const Item& item, int row, int lane)
 {
     constexpr int ROWS = 16 * CB, kEach = D / 64;
-    const int lane = threadIdx.x & 63, row = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int count = items[0].parts;
-    const Item item = items[1 + blockIdx.x];                             // (of the last call, or nothing, from the count on)
-    if (blockIdx.x >= count || item.parts <= 1 || item.row0 + row >= item.rows) return;
     float top = kNothing, sum = 0.0f, acc[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) acc[i] = 0.0f;
@@ -637,6 +633,20 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
     else *dst = __float2half_rn(acc[0] * f);
 }
 
+// Adds the partial sums of the histories that were cut: a workgroup takes four rows of one, one to a wavefront.
+constexpr int kJoinGroups = 1 << 16;     // (there may be more histories than a launch can have workgroups)
+template <int D, int CB>
+__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items)
+{
+    const int lane = threadIdx.x & 63, row = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int count = items[0].parts;
+    Item item = items[1 + blockIdx.x];                                   // (of the last call, or nothing, from the count on)
+    for (int64_t i = blockIdx.x; i < count; i += gridDim.x) {
+        if (i != blockIdx.x) item = items[1 + i];
+        if (item.parts > 1 && item.row0 + row < item.rows) join<D, CB>(a, partial, item, row, lane);
+    }
+}
+
 // What a call has at most: histories (of 16 rows), and workgroups with something to do.
 struct Most {
     int64_t items, groups;
@@ -666,7 +676,7 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
     float* const partial = static_cast<float*>(ws);
     Item* const items = reinterpret_cast<Item*>(static_cast<uint8_t*>(ws) + partial_bytes(most.groups, D, CB));
     kernel<<<(unsigned)groups, kThreads, lds, st>>>(a, partial, items, most.items, small_rows);
-    k_kv4_attention_join<D, CB><<<dim3((unsigned)most.items, 4 * CB), kThreads, 0, st>>>(a, partial, items);
+    k_kv4_attention_join<D, CB><<<dim3((unsigned)(most.items < kJoinGroups ? most.items : kJoinGroups), 4 * CB), kThreads, 0, st>>>(a, partial, items);
     return hip_status(hipGetLastError());
 }
 
