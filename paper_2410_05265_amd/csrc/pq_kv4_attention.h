@@ -72,6 +72,9 @@ __device__ __forceinline__ float add_halves(uint32_t pair, float to)
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, pair), one, to, false);
 }
 
+// 1 / x of a power of two.
+__device__ __forceinline__ float inverse(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
+
 // A request as the kernels see it: nothing that lies on the device takes them out of bounds.
 struct Request {
     int32_t start, q_len, n;     // first row, rows, cached tokens

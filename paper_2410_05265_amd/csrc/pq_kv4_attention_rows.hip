@@ -396,6 +396,11 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             const bool masked = t0 + kTile > all_see || bad0 || bad1;
             uint32_t k[2][NG * KS], v[8][NG];
             v4f ks[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1], vs[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1];
+            // (steps of four tokens, NG each, one after another; every 32 steps of keys are followed by 32 of values)
+            auto steps = [&](int blk, int j) PQ_INLINE {
+                const int e = (16 * blk + 4 * quarter) * NG + 4 * j;
+                return kc + 2 * S::CODES + e / 32 * 256 + e % 32 * 4;
+            };
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
@@ -412,28 +417,28 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                     } else {
                         k[blk][g] = *reinterpret_cast<const uint32_t*>(src);
                     }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint8_t* from_v = vc + (16 * blk + 4 * quarter + j) * (D / 2) + g * (G / 2) + col * (G / 32);
-                        if constexpr (KS == 4) v[4 * blk + j][g] = *reinterpret_cast<const uint32_t*>(from_v);
-                        else if constexpr (KS == 2) v[4 * blk + j][g] = *reinterpret_cast<const uint16_t*>(from_v);
-                        else v[4 * blk + j][g] = *from_v;
-                    }
+                    if constexpr (DYNAMIC) ks[blk][g] = *reinterpret_cast<const v4f*>(steps(blk, g));
                 }
-            if constexpr (DYNAMIC) {
-                // steps of four tokens, NG each, one after another; every 32 steps of keys are followed by 32 of values
+            auto values = [&]() PQ_INLINE {
 #pragma unroll
                 for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-                    for (int j = 0; j < NG; ++j) {
-                        const int e = (16 * blk + 4 * quarter) * NG + 4 * j;
-                        const uint8_t* src = kc + 2 * S::CODES + e / 32 * 256 + e % 32 * 4;
-                        ks[blk][j] = *reinterpret_cast<const v4f*>(src);
-                        vs[blk][j] = *reinterpret_cast<const v4f*>(src + 128);
+                    for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint8_t* from_v = vc + (16 * blk + 4 * quarter + j) * (D / 2) + g * (G / 2) + col * (G / 32);
+                            if constexpr (KS == 4) v[4 * blk + j][g] = *reinterpret_cast<const uint32_t*>(from_v);
+                            else if constexpr (KS == 2) v[4 * blk + j][g] = *reinterpret_cast<const uint16_t*>(from_v);
+                            else v[4 * blk + j][g] = *from_v;
+                        }
+                        if constexpr (DYNAMIC) vs[blk][g] = *reinterpret_cast<const v4f*>(steps(blk, g) + 128);
                     }
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // read before the next tile takes this place
-            if (i + kDepth < count) fetch(i + kDepth);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // read before the next tile takes this place
+                if (i + kDepth < count) fetch(i + kDepth);
+            };
+            // (four groups, or two and two blocks of rows: keys and values at once would not fit the registers)
+            constexpr bool kLater = NG * CB >= 4;
+            if constexpr (!kLater) values();
 
             float x[CB][8];
             v4u pr[CB];
@@ -470,6 +475,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             }
 #pragma unroll
             for (int c = 0; c < CB; ++c) probabilities(c, x[c], c1, DYNAMIC ? 0.0f : c0[c][0] * c1, pr[c]);
+            if constexpr (kLater) values();
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 if constexpr (DYNAMIC) {
@@ -485,7 +491,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 #pragma unroll
                     for (int c = 0; c < CB; ++c) {
                         float w[8], most = 0.0f;
-                        const float inv = 1.0f / ref[c][g];              // a power of two
+                        const float inv = inverse(ref[c][g]);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             w[j] = x[c][j] * inv * step[j];
@@ -683,8 +689,10 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
 // Column blocks: one, if it holds every request's rows (max_q is right, or more tiles of rows are taken).
 int blocks_for(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv <= 16 ? 1 : 2; }
 
-// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and this one the others.
-constexpr int kSmallRows = 64;
+// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and this one the others.  This | tile kernel, us,
+// 32 heads of 128 on 8: one request of 33000 tokens with 128 rows 56 | 107, 192 63 | 110, 256 77 | 79; 8 of up to 4000 46 | 63, 52 | 54,
+// 60 | 55; 64 of up to 2000 113 | 137, 146 | 140, 185 | 148; with a step to 32 channels 218 | 307, 284 | 322, 372 | 330.
+constexpr int kSmallRows = 192;
 
 bool takes_tiles(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv > kSmallRows; }
 int small_rows_for(int32_t max_q, int32_t per_kv) { return takes_tiles(max_q, per_kv) ? kSmallRows : INT32_MAX; }

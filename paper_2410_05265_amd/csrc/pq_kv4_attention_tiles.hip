@@ -85,12 +85,21 @@ template <int G> __device__ __forceinline__ constexpr int place_of(int channel)
     return channel - in + (in % 8) * (G / 8) + in / 8;
 }
 
+// Operands of codes, u * 2^-20, without their offset: (u - 8) * 2^-20, exact in fp16.  With dynamic steps the offset would cost a sum of the
+// weights for every group of channels and an addition to every score; here it is taken off once for all eight wavefronts.
+template <int N, typename V> __device__ __forceinline__ V without_offset(const V& x)
+{
+    typedef _Float16 halves __attribute__((ext_vector_type(N)));
+    return __builtin_bit_cast(V, __builtin_bit_cast(halves, x) - (halves)(_Float16)0x1.0p-17f);
+}
+
 template <int D, int G, bool DYNAMIC>
 struct Lds {
     static constexpr int NG = D / G;
     v4u k[2][kTile][D / 8 + 1];          // [token][eight channels]; tokens an odd number of 16 bytes apart, so that eight of them meet all banks
     v2u v[2][kTile / 16][2][D][2];       // [16 tokens][half of the lanes][channel]: eight tokens in the order of the probabilities
     float ks[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1][kTile], vs[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1][kTile];
+    float vs_most[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1][4];     // largest of a block of 16 tokens
     int bad[2][4];                       // blocks of 16 tokens whose page is none
 };
 
@@ -118,7 +127,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
     // this lane's query
     int limit, wave_sees = r.n;              // tokens that it sees, and that all of the wavefront's see
     v8h q[KS];
-    float c0[NG];
+    float c0 = 0.0f;                         // -8 sum(q): the codes' offset (dynamic steps: the operands are without it)
     {
         const int row = min(row0 + wave * kCols + col, rows - 1);
         const int token = row / per_kv, q_head = head * per_kv + row % per_kv;
@@ -126,14 +135,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
         if (a.causal) wave_sees = r.n - (r.q_len - 1 - min(row0 + wave * kCols, rows - 1) / per_kv);
         const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = in_key_order(*reinterpret_cast<const v4u*>(src + 16 * s + 8 * half));
-        const v4u minus8 = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
+        for (int s = 0; s < KS; ++s)
+            q[s] = in_key_order(*reinterpret_cast<const v4u*>(src + 16 * s + 8 * half));
+        if constexpr (!DYNAMIC) {
+            const v4u minus8 = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
             v16f z = {};
 #pragma unroll
-            for (int s = 0; s < KSG; ++s) z = product(__builtin_bit_cast(v8h, minus8), q[g * KSG + s], z);
-            c0[g] = z[0];
+            for (int s = 0; s < KS; ++s) z = product(__builtin_bit_cast(v8h, minus8), q[s], z);
+            c0 = z[0];
         }
     }
     const float scale = a.softmax_scale * 1.44269504088896341f;
@@ -144,15 +153,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
     }
 
     float m = kNothing, l = 0.0f;
-    float ref[NG], lw[NG];
+    float ref[NG];                           // dynamic steps: weights p * step are rounded relative to ref
     v16f o[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] = (v16f){};
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-        ref[g] = kLeast;
-        lw[g] = 0.0f;
-    }
+    for (int g = 0; g < NG; ++g) ref[g] = kLeast;
 
     // exp2(c1 x + bias - m) of a tile's scores.  The reference m follows the largest; what is there is rescaled.
     auto probabilities = [&](float (&x)[32], float c1, float bias, v4u (&p)[4]) PQ_INLINE {
@@ -171,7 +177,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
                 for (int g = 0; g < NG; ++g) {
                     const float y = ref[g] * alpha, f = y >= kLeast ? 1.0f : y * (1.0f / kLeast);
                     ref[g] = fmaxf(y, kLeast);
-                    lw[g] *= f;
 #pragma unroll
                     for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
                 }
@@ -190,48 +195,44 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
             l = add_halves(two, l);
         }
     };
-    // dynamic steps: the weights p * step of one group, rounded relative to ref
-    auto weights = [&](int buf, int g, const float (&x)[32], v4u (&p)[4]) PQ_INLINE {
-        const float inv = 1.0f / ref[g];           // a power of two
-        float w[32], most = 0.0f;
+    // dynamic steps: the weights p * step of one group, rounded relative to ref, which moves as m does
+    auto weights = [&](int buf, int g, const float (&x)[32], float most_x, v4u (&p)[4]) PQ_INLINE {
+        const v4f most4 = *reinterpret_cast<const v4f*>(&sh.vs_most[buf][g][0]);
+        const float most_step = fmaxf(fmaxf(most4[0], most4[1]), fmaxf(most4[2], most4[3]));
+        // no weight is larger than this product
+        if (__builtin_amdgcn_ballot_w64(most_x * most_step > 0x1.0p14f * ref[g]) != 0) {
+            float most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
+            for (int i = 0; i < 32; i += 4) {
+                const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                // (a token that is not seen weighs nothing, whatever its step is)
-                w[i + j] = x[i + j] > 0.0f ? x[i + j] * inv * step[j] : 0.0f;
-                most = fmaxf(most, w[i + j]);
+                for (int j = 0; j < 4; ++j) most = fmaxf(most, x[i + j] * step[j]);
             }
-        }
-        if (__builtin_amdgcn_ballot_w64(most > 0x1.0p14f) != 0) {
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64)) * inverse(ref[g]);
             const int up = most > 0x1.0p14f ? ilogbf(most) - (int)kBack : 0;
             const float f = ldexpf(1.0f, -up);
             ref[g] = ldexpf(ref[g], up);
-            lw[g] *= f;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) w[i] *= f;
 #pragma unroll
             for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
         }
+        const float inv = inverse(ref[g]);
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            const uint32_t two = two_halves(w[i], w[i + 1]);
-            p[i >> 3][(i & 7) >> 1] = two;
-            lw[g] = add_halves(two, lw[g]);
+        for (int i = 0; i < 32; i += 4) {
+            const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
+            p[i >> 3][(i & 7) >> 1] = two_halves(x[i] * inv * step[0], x[i + 1] * inv * step[1]);
+            p[i >> 3][((i & 7) >> 1) + 1] = two_halves(x[i + 2] * inv * step[2], x[i + 3] * inv * step[3]);
         }
     };
     // scores x of a tile [token 32 tb + 8 (i / 4) + 4 half + i % 4], in units of a code (dynamic: of 2^20 steps)
     auto scores = [&](int buf, float (&x)[32]) PQ_INLINE {
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
+        for (int g = 0; g < NG; ++g) {
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
+            for (int tb = 0; tb < 2; ++tb) {
                 v16f z = {};
 #pragma unroll
-                for (int k = g * KSG; k < (g + 1) * KSG; ++k)
-                    z = product(__builtin_bit_cast(v8h, sh.k[buf][32 * tb + col][2 * k + half]), q[k], z);
+                for (int k = 0; k < KSG; ++k)
+                    z = product(__builtin_bit_cast(v8h, sh.k[buf][32 * tb + col][2 * (g * KSG + k) + half]), q[g * KSG + k], z);
                 if constexpr (DYNAMIC) {
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
@@ -239,14 +240,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             float& to = x[16 * tb + i + j];
-                            to = fmaf(z[i + j] + c0[g], step[j], g == 0 ? 0.0f : to);
+                            to = g == 0 ? z[i + j] * step[j] : fmaf(z[i + j], step[j], to);
                         }
                     }
+                    // (computed here, and not sunk to where the scores are used: all groups' products and steps would not fit the registers)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(x[16 * tb + i]));
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[16 * tb + i] = z[i];
                 }
             }
+        }
     };
     auto multiply = [&](int buf, int first, int count, const v4u (&p)[4]) PQ_INLINE {
 #pragma unroll
@@ -258,12 +263,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
 
     // ---- prefix tokens: as a tile of their own, in fp16
     if (a.n_prefix > 0 && split == 0) {
-        float keep[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            keep[g] = c0[g];
-            c0[g] = 0.0f;
-        }
         for (int t0 = 0; t0 < a.n_prefix; t0 += kTile) {
             __syncthreads();
             for (int i = tid; i < kTile * (D / 8); i += kThreads) {
@@ -305,10 +304,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = fmaf(o[d][i], times, plus);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            ref[g] = kLeast;
-            c0[g] = keep[g];
-        }
+        for (int g = 0; g < NG; ++g) ref[g] = kLeast;
     }
 
     // ---- the history: wavefronts w and w + 4 load and expand keys and values of tokens 16 w .. 16 w + 15 of every tile
@@ -348,7 +344,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
         const int t = 16 * block + (lane >> 2);
         if (keys) {
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) sh.k[buf][t][(lane & 3) * (D / 32) + i] = __builtin_bit_cast(v4u, key_operand(x.w[i]));
+            for (int i = 0; i < D / 32; ++i) sh.k[buf][t][(lane & 3) * (D / 32) + i] =
+                DYNAMIC ? without_offset<8>(__builtin_bit_cast(v4u, key_operand(x.w[i]))) : __builtin_bit_cast(v4u, key_operand(x.w[i]));
             if (lane == 0) sh.bad[buf][block] = x.bad;
             if constexpr (DYNAMIC) {
                 if ((lane & 3) < NG) sh.ks[buf][lane & 3][t] = x.s;
@@ -366,11 +363,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
                 constexpr int j = decltype(J)::value;
                 const uint32_t* const w = j < 4 ? low : high;
                 const v2u y = {operand<(j & 3)>(w[0]), operand<(j & 3)>(w[1])};
-                sh.v[buf][block][quad & 1][place_of<G>(D / 16 * c + j)][quad >> 1] = y;
+                sh.v[buf][block][quad & 1][place_of<G>(D / 16 * c + j)][quad >> 1] = DYNAMIC ? without_offset<4>(y) : y;
             });
             if constexpr (DYNAMIC) {
-                // what lies behind the last token may be anything: it must not meet a probability of zero
-                if ((lane & 3) < NG) sh.vs[buf][lane & 3][t] = tile * kTile + t < r.n ? x.s : 0.0f;
+                // what lies behind the last token, or in no page, may be anything: it must not meet a probability of zero
+                const float step = tile * kTile + t < r.n && !x.bad ? x.s : 0.0f;
+                float most = step;
+#pragma unroll
+                for (int d = 4; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+                if ((lane & 3) < NG) sh.vs[buf][lane & 3][t] = step;
+                if (lane < NG) sh.vs_most[buf][lane][block] = most;
             }
         }
     };
@@ -379,7 +381,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
         Codes next;
         load(begin, page_of(begin), next);
         int page = page_of(begin + 1);
-        const float bias = DYNAMIC ? 0.0f : c0[0] * c1;
+        const float bias = c0 * c1;
         expand(begin, 0, next);
         load(begin + 1, page, next);
         page = page_of(begin + 2);
@@ -403,10 +405,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
             }
             probabilities(x, c1, bias, p);
             if constexpr (DYNAMIC) {
+                float most_x = x[0];
+#pragma unroll
+                for (int i = 1; i < 32; ++i) most_x = fmaxf(most_x, x[i]);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    weights(buf, g, x, p);
+                    weights(buf, g, x, most_x, p);
                     multiply(buf, g * DBG, DBG, p);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
                 multiply(buf, 0, DB, p);
@@ -416,15 +422,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
 
     // ---- results
     const float l_all = l + __shfl_xor(l, 32, 64);
-    float times[NG], minus[NG];
+    float times[NG], minus = 0.0f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         if constexpr (DYNAMIC) {
             times[g] = kUnit * ref[g];
-            minus[g] = 8.0f * ref[g] * (lw[g] + __shfl_xor(lw[g], 32, 64));
         } else {
             times[g] = kUnit * v_step;
-            minus[g] = 8.0f * v_step * l_all;
+            minus = 8.0f * v_step * l_all;
         }
     }
     if (splits > 1) {
@@ -434,7 +439,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                dst[(32 * d + 8 * (i >> 2) + 4 * half + (i & 3)) * kRows] = fmaf(o[d][i], times[d / DBG], -minus[d / DBG]);
+                dst[(32 * d + 8 * (i >> 2) + 4 * half + (i & 3)) * kRows] = fmaf(o[d][i], times[d / DBG], -minus);
         if (half == 0) {
             dst[D * kRows] = m;
             dst[(D + 1) * kRows] = l_all;
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             lines[col * (D + 8) + channel_of<G>(32 * d + 8 * (i >> 2) + 4 * half + (i & 3))] =
-                __float2half_rn(fmaf(o[d][i], times[d / DBG], -minus[d / DBG]) * f);
+                __float2half_rn(fmaf(o[d][i], times[d / DBG], -minus) * f);
     // (each wavefront its own rows: what it reads here it has written itself)
     constexpr int kPer = D / 8;                    // lanes to a row
     for (int i = lane / kPer; i < kCols; i += 64 / kPer) {
@@ -498,16 +503,28 @@ __global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_tiles(Atten
     }
 }
 
-int64_t tiles_at_most(int64_t T, int32_t B, int32_t per_kv) { return T * per_kv / kRows + B; }
+int64_t tiles_at_most(int64_t T, int32_t B, int32_t per_kv) { return (T * per_kv + (int64_t)(kRows - 1) * B) / kRows; }
 
-// Parts of a history: as many as bring the tiles to the compute units, and no longer than to leave each some tiles of tokens.
-int splits_for(int64_t tiles, int32_t n_kv_heads, int64_t capacity)
+// Parts of a history, of at least eight tiles of tokens each.  Several requests differ in length: about two workgroups to a CU even that
+// out (B 4, 300 queries each over up to 4000 tokens, 32 on 8 heads: one part 127 us, two 103, three 112).  The parts of one request are
+// alike: as many as fill whole rounds of one workgroup to a CU, which is what its registers allow, with eight tiles' time for what every
+// workgroup does once (500 queries over 33000 tokens, 64 on 8 heads: one part 910 us, two 534, four 541; 64 queries over 131072, 32 on 8
+// heads: 16 parts 269, 32 173, 64 202; 400 queries over 20000, 8 heads on one: 19 parts 75, 39 91).
+int splits_for(int64_t tiles, int32_t B, int32_t n_kv_heads, int64_t capacity)
 {
-    const int64_t groups = tiles * n_kv_heads;
-    int64_t s = 512 / (groups > 0 ? groups : 1);
-    const int64_t most = capacity / (8 * kTile);
-    if (s > most) s = most;
-    return s > 1 ? (int)s : 1;
+    const int64_t groups = tiles * n_kv_heads, steps = capacity / kTile, most = steps / 8 < 512 / groups ? steps / 8 : 512 / groups;
+    if (most <= 1) return 1;
+    if (B > 1) return (int)most;
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; s <= (int)most; ++s) {
+        const double time = (double)((groups * s + 255) / 256) * ((double)steps / s + 8.0);
+        if (time < least) {
+            least = time;
+            best = s;
+        }
+    }
+    return best;
 }
 
 template <int D, int G, bool DYNAMIC>
@@ -528,14 +545,14 @@ int launch(const AttentionArgs& a, int64_t tiles, int splits, int small_rows, fl
 size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity)
 {
     const int64_t tiles = tiles_at_most(T, B, n_heads / n_kv_heads);
-    const int splits = splits_for(tiles, n_kv_heads, capacity);
+    const int splits = splits_for(tiles, B, n_kv_heads, capacity);
     return splits > 1 ? (size_t)(tiles * n_kv_heads * splits) * kRows * (head_dim + 2) * sizeof(float) : 0;
 }
 
 int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st)
 {
     const int64_t tiles = tiles_at_most(a.T, a.B, a.heads_per_kv);
-    const int splits = splits_for(tiles, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
+    const int splits = splits_for(tiles, a.B, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
     if (head_dim == 64) {
         if (group == 0) return launch<64, 64, false>(a, tiles, splits, small_rows, partial, st);
         if (group == 32) return launch<64, 32, true>(a, tiles, splits, small_rows, partial, st);
