@@ -584,59 +584,67 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
     }
 }
 
-// Row `row` of one history that was cut, by a wavefront.
+// Row `row` of one history that was cut, by a wavefront: two channels (one of 64) and one part's maximum and sum to a lane.
+template <int D> struct Joined {
+    float top = kNothing, sum = 0.0f, acc[D / 64] = {};
+};
+
+// The next COUNT or fewer parts.  All their loads are on their way before the first is used: one after another they would take a microsecond
+// each, and a second one if they waited for the maxima.
+template <int D, int COUNT>
+__device__ __forceinline__ void add_parts(Joined<D>& j, const float* __restrict__ first, int64_t step, int64_t second, int n0, int n, int lane)
+{
+    constexpr int kEach = D / 64;
+    float x[COUNT][kEach];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const int at = n0 + min(i, n - 1);
+        const float* src = first + at * step + (at == 0 ? second : 0) + 4 + kEach * lane;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) x[i][k] = src[k];
+    }
+    const int mine = n0 + min(lane, n - 1);
+    const float* const head = first + mine * step + (mine == 0 ? second : 0);
+    const float m = lane < n ? head[0] : kNothing, l = lane < n ? head[1] : 0.0f;
+    float to = m;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d, 64));
+    to = fmaxf(to, j.top);
+    const float old = __builtin_amdgcn_exp2f(j.top - to), f = lane < n ? __builtin_amdgcn_exp2f(m - to) : 0.0f;
+    float part = l * f;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d, 64);
+    j.sum = fmaf(j.sum, old, part);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) j.acc[k] *= old;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const float fi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i));
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) j.acc[k] = fmaf(x[i][k], fi, j.acc[k]);
+    }
+    j.top = to;
+}
+
 template <int D, int CB>
 __device__ __forceinline__ void join(const AttentionArgs& a, const float* __restrict__ partial, const Item& item, int row, int lane)
 {
     constexpr int ROWS = 16 * CB, kEach = D / 64;
-    float top = kNothing, sum = 0.0f, acc[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) acc[i] = 0.0f;
+    Joined<D> j;
     const float* const first = partial + ((int64_t)item.worker * 2 * ROWS + row) * (D + 4);
     const int64_t step = 2 * ROWS * (D + 4), second = item.second ? ROWS * (D + 4) : 0;
-    for (int n0 = 0; n0 < item.parts; n0 += 64) {
-        const int n = min(item.parts - n0, 64), mine = n0 + min(lane, n - 1);
-        const float* const head = first + mine * step + (mine == 0 ? second : 0);
-        const float m = lane < n ? head[0] : kNothing, l = lane < n ? head[1] : 0.0f;
-        float to = m;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d, 64));
-        to = fmaxf(to, top);
-        const float old = __builtin_amdgcn_exp2f(top - to), f = __builtin_amdgcn_exp2f(m - to);
-        float part = lane < n ? l * f : 0.0f;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d, 64);
-        sum = fmaf(sum, old, part);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) acc[i] *= old;
-        // loads of up to 32 parts at once: one after another they would take a microsecond each
-        auto add = [&](int i0, auto COUNT) PQ_INLINE {
-            constexpr int kCount = decltype(COUNT)::value;
-            float x[kCount][kEach];
-#pragma unroll
-            for (int i = 0; i < kCount; ++i) {
-                const int at = n0 + min(i0 + i, n - 1);
-                const float* src = first + at * step + (at == 0 ? second : 0) + 4 + kEach * lane;
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) x[i][k] = src[k];
-            }
-#pragma unroll
-            for (int i = 0; i < kCount; ++i) {
-                const float fi = __shfl(f, min(i0 + i, n - 1), 64);
-#pragma unroll
-                for (int k = 0; k < kEach; ++k) acc[k] = fmaf(x[i][k], i0 + i < n ? fi : 0.0f, acc[k]);
-            }
-        };
-        int i0 = 0;
-        for (; n - i0 > 8; i0 += 32) add(i0, std::integral_constant<int, 32>{});
-        if (i0 < n) add(i0, std::integral_constant<int, 8>{});
-        top = to;
+    int n0 = 0;
+    for (; item.parts - n0 > 8; n0 += 64) {
+        const int n = min(item.parts - n0, 64);
+        if (n > 32) add_parts<D, 64>(j, first, step, second, n0, n, lane);
+        else add_parts<D, 32>(j, first, step, second, n0, n, lane);
     }
-    const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+    if (n0 < item.parts) add_parts<D, 8>(j, first, step, second, n0, item.parts - n0, lane);
+    const float f = j.sum > 0.0f ? 1.0f / j.sum : 0.0f;
     const int at_row = item.row0 + row, per_kv = a.heads_per_kv;
     __half* dst = a.out + ((int64_t)(item.start + at_row / per_kv) * a.n_heads + item.head * per_kv + at_row % per_kv) * D + kEach * lane;
-    if constexpr (kEach == 2) *reinterpret_cast<__half2*>(dst) = __floats2half2_rn(acc[0] * f, acc[1] * f);
-    else *dst = __float2half_rn(acc[0] * f);
+    if constexpr (kEach == 2) *reinterpret_cast<__half2*>(dst) = __floats2half2_rn(j.acc[0] * f, j.acc[1] * f);
+    else *dst = __float2half_rn(j.acc[0] * f);
 }
 
 // Adds the partial sums of the histories that were cut: a workgroup takes four rows of one, one to a wavefront.
