@@ -41,8 +41,12 @@ __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r
 __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index, int small_rows, int lane)
 {
     const int each = (a.B + 63) / 64, first = min(lane * each, a.B), last = min(first + each, a.B);
+    Request r = {0, 0, 0};                         // the last of this lane's; up to 64 requests are read once
     int64_t own = 0;
-    for (int b = first; b < last; ++b) own += tiles_of(a, request(a, b), small_rows);
+    for (int b = first; b < last; ++b) {
+        r = request(a, b);
+        own += tiles_of(a, r, small_rows);
+    }
     int64_t incl = own;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -51,13 +55,13 @@ __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index
     }
     const bool mine = incl - own <= index && index < incl;
     const uint64_t found = __builtin_amdgcn_ballot_w64(mine);
-    Where w = {-1, 0, {0, 0, 0}};
-    if (found == 0) return w;
-    int b = first, tile = 0;
-    if (mine) {
+    if (found == 0) return {-1, 0, r};
+    int b = first, tile = (int)(incl - 1 - index);
+    if (mine && last - first > 1) {
         int64_t u = incl - own;
         for (; b < last; ++b) {
-            const int n = tiles_of(a, request(a, b), small_rows);
+            r = request(a, b);
+            const int n = tiles_of(a, r, small_rows);
             if (index < u + n) {
                 tile = (int)(u + n - 1 - index);
                 break;
@@ -66,10 +70,8 @@ __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index
         }
     }
     const int from = __builtin_ctzll(found);
-    w.b = __builtin_amdgcn_readfirstlane(__shfl(b, from, 64));
-    w.tile = __builtin_amdgcn_readfirstlane(__shfl(tile, from, 64));
-    w.r = request(a, w.b);
-    return w;
+    auto lanes = [&](int v) PQ_INLINE { return __builtin_amdgcn_readlane(v, from); };
+    return {lanes(b), lanes(tile), {lanes(r.start), lanes(r.q_len), lanes(r.n)}};
 }
 
 // Row `at` of the accumulators as a channel: channels of a group lie so in LDS that neighbouring threads of the expansion write
@@ -261,52 +263,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
                 o[d] = product(*reinterpret_cast<const v8h*>(&sh.v[buf][k][half][32 * d + col][0]), __builtin_bit_cast(v8h, p[k]), o[d]);
     };
 
-    // ---- prefix tokens: as a tile of their own, in fp16
-    if (a.n_prefix > 0 && split == 0) {
-        for (int t0 = 0; t0 < a.n_prefix; t0 += kTile) {
-            __syncthreads();
-            for (int i = tid; i < kTile * (D / 8); i += kThreads) {
-                const int t = i / (D / 8), c = i % (D / 8);
-                const int64_t from = ((int64_t)min(t0 + t, a.n_prefix - 1) * Hkv + head) * D + 8 * c;
-                sh.k[0][t][c] = __builtin_bit_cast(v4u, in_key_order(*reinterpret_cast<const v4u*>(a.prefix_k + from)));
-                const v4u x = *reinterpret_cast<const v4u*>(a.prefix_v + from);
-                // token t of its 16: 8 (t / 8) + 4 (half of the lanes) + t % 4
-                const int in16 = t & 15;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    __half* dst = reinterpret_cast<__half*>(&sh.v[0][t >> 4][(in16 >> 2) & 1][place_of<G>(8 * c + j)][in16 >> 3]);
-                    dst[in16 & 3] = reinterpret_cast<const __half*>(&x)[j];
-                }
-            }
-            if constexpr (DYNAMIC) {
-                if (tid < kTile) {
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) sh.ks[0][g][tid] = 1.0f;
-                }
-            }
-            __syncthreads();
-            float x[32];
-            v4u p[4];
-            scores(0, x);
-            const int left = a.n_prefix - t0 - 4 * half;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (8 * (i >> 2) + (i & 3) >= left) x[i] = -INFINITY;
-            probabilities(x, scale, 0.0f, p);
-            multiply(0, 0, DB, p);
-        }
-        __syncthreads();
-        // as if they were codes: sum p v = step (unit acc - 8 sum p) has to hold
-        const float l_all = l + __shfl_xor(l, 32, 64);
-        const float times = DYNAMIC ? 1.0f / (kUnit * kLeast) : 1.0f / (kUnit * v_step), plus = DYNAMIC ? 0.0f : 8.0f / kUnit * l_all;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = fmaf(o[d][i], times, plus);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) ref[g] = kLeast;
-    }
-
     // ---- the history: wavefronts w and w + 4 load and expand keys and values of tokens 16 w .. 16 w + 15 of every tile
     const int32_t* table = a.table + (int64_t)at.b * a.table_pages;
     const int block = wave & 3;
@@ -377,10 +333,60 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
         }
     };
 
-    if (begin < end) {
-        Codes next;
+    Codes next;
+    int page = 0;
+    if (begin < end) {                             // (on their way while the prefix tokens are taken)
         load(begin, page_of(begin), next);
-        int page = page_of(begin + 1);
+        page = page_of(begin + 1);
+    }
+
+    // ---- prefix tokens: as a tile of their own, in fp16
+    if (a.n_prefix > 0 && split == 0) {
+        for (int t0 = 0; t0 < a.n_prefix; t0 += kTile) {
+            __syncthreads();
+            for (int i = tid; i < kTile * (D / 8); i += kThreads) {
+                const int t = i / (D / 8), c = i % (D / 8);
+                const int64_t from = ((int64_t)min(t0 + t, a.n_prefix - 1) * Hkv + head) * D + 8 * c;
+                sh.k[0][t][c] = __builtin_bit_cast(v4u, in_key_order(*reinterpret_cast<const v4u*>(a.prefix_k + from)));
+                const v4u x = *reinterpret_cast<const v4u*>(a.prefix_v + from);
+                // token t of its 16: 8 (t / 8) + 4 (half of the lanes) + t % 4
+                const int in16 = t & 15;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    __half* dst = reinterpret_cast<__half*>(&sh.v[0][t >> 4][(in16 >> 2) & 1][place_of<G>(8 * c + j)][in16 >> 3]);
+                    dst[in16 & 3] = reinterpret_cast<const __half*>(&x)[j];
+                }
+            }
+            if constexpr (DYNAMIC) {
+                if (tid < kTile) {
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) sh.ks[0][g][tid] = 1.0f;
+                }
+            }
+            __syncthreads();
+            float x[32];
+            v4u p[4];
+            scores(0, x);
+            const int left = a.n_prefix - t0 - 4 * half;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (8 * (i >> 2) + (i & 3) >= left) x[i] = -INFINITY;
+            probabilities(x, scale, 0.0f, p);
+            multiply(0, 0, DB, p);
+        }
+        __syncthreads();
+        // as if they were codes: sum p v = step (unit acc - 8 sum p) has to hold
+        const float l_all = l + __shfl_xor(l, 32, 64);
+        const float times = DYNAMIC ? 1.0f / (kUnit * kLeast) : 1.0f / (kUnit * v_step), plus = DYNAMIC ? 0.0f : 8.0f / kUnit * l_all;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = fmaf(o[d][i], times, plus);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) ref[g] = kLeast;
+    }
+
+    if (begin < end) {
         const float bias = c0 * c1;
         expand(begin, 0, next);
         load(begin + 1, page, next);
