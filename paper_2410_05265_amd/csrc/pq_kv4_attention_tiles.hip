@@ -21,6 +21,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 512, kWaves = 8;
 constexpr int kRows = kTileRows, kCols = 32;      // rows of a workgroup and of a wavefront
 constexpr int kTile = 64;                         // tokens of a step
+constexpr int kPrefixTile = 32;
 constexpr int kJoinThreads = 256;
 constexpr float kLeast = 0x1.0p-80f;
 
@@ -137,132 +138,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
         if (a.causal) wave_sees = r.n - (r.q_len - 1 - min(row0 + wave * kCols, rows - 1) / per_kv);
         const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-            q[s] = in_key_order(*reinterpret_cast<const v4u*>(src + 16 * s + 8 * half));
-        if constexpr (!DYNAMIC) {
-            const v4u minus8 = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-            v16f z = {};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) z = product(__builtin_bit_cast(v8h, minus8), q[s], z);
-            c0 = z[0];
-        }
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h*>(src + 16 * s + 8 * half);
     }
-    const float scale = a.softmax_scale * 1.44269504088896341f;
-    float c1 = scale * kUnit, v_step = 1.0f;
-    if constexpr (!DYNAMIC) {
-        c1 *= a.cache.k_scale[head];
-        v_step = a.cache.v_scale[head];
-    }
-
-    float m = kNothing, l = 0.0f;
-    float ref[NG];                           // dynamic steps: weights p * step are rounded relative to ref
-    v16f o[DB];
-#pragma unroll
-    for (int i = 0; i < DB; ++i) o[i] = (v16f){};
-#pragma unroll
-    for (int g = 0; g < NG; ++g) ref[g] = kLeast;
-
-    // exp2(c1 x + bias - m) of a tile's scores.  The reference m follows the largest; what is there is rescaled.
-    auto probabilities = [&](float (&x)[32], float c1, float bias, v4u (&p)[4]) PQ_INLINE {
-        float most = x[0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) most = fmaxf(most, x[i]);
-        most = fmaf(most, c1, bias);
-        if (__builtin_amdgcn_ballot_w64(most > m + kMost) != 0) {
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            const float to_m = most > m + kMost ? ceilf(most) - kBack : m;
-            const float alpha = __builtin_amdgcn_exp2f(m - to_m);
-            m = to_m;
-            l *= alpha;
-            if constexpr (DYNAMIC) {
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const float y = ref[g] * alpha, f = y >= kLeast ? 1.0f : y * (1.0f / kLeast);
-                    ref[g] = fmaxf(y, kLeast);
-#pragma unroll
-                    for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < DB; ++i) o[i] *= alpha;
-            }
-        }
-        const float minus = bias - m;
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c1, minus));
-            x[i + 1] = __builtin_amdgcn_exp2f(fmaf(x[i + 1], c1, minus));
-            const uint32_t two = two_halves(x[i], x[i + 1]);
-            p[i >> 3][(i & 7) >> 1] = two;
-            l = add_halves(two, l);
-        }
-    };
-    // dynamic steps: the weights p * step of one group, rounded relative to ref, which moves as m does
-    auto weights = [&](int buf, int g, const float (&x)[32], float most_x, v4u (&p)[4]) PQ_INLINE {
-        const v4f most4 = *reinterpret_cast<const v4f*>(&sh.vs_most[buf][g][0]);
-        const float most_step = fmaxf(fmaxf(most4[0], most4[1]), fmaxf(most4[2], most4[3]));
-        // no weight is larger than this product
-        if (__builtin_amdgcn_ballot_w64(most_x * most_step > 0x1.0p14f * ref[g]) != 0) {
-            float most = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) most = fmaxf(most, x[i + j] * step[j]);
-            }
-            most = fmaxf(most, __shfl_xor(most, 32, 64)) * inverse(ref[g]);
-            const int up = most > 0x1.0p14f ? ilogbf(most) - (int)kBack : 0;
-            const float f = ldexpf(1.0f, -up);
-            ref[g] = ldexpf(ref[g], up);
-#pragma unroll
-            for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
-        }
-        const float inv = inverse(ref[g]);
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
-            p[i >> 3][(i & 7) >> 1] = two_halves(x[i] * inv * step[0], x[i + 1] * inv * step[1]);
-            p[i >> 3][((i & 7) >> 1) + 1] = two_halves(x[i + 2] * inv * step[2], x[i + 3] * inv * step[3]);
-        }
-    };
-    // scores x of a tile [token 32 tb + 8 (i / 4) + 4 half + i % 4], in units of a code (dynamic: of 2^20 steps)
-    auto scores = [&](int buf, float (&x)[32]) PQ_INLINE {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-                v16f z = {};
-#pragma unroll
-                for (int k = 0; k < KSG; ++k)
-                    z = product(__builtin_bit_cast(v8h, sh.k[buf][32 * tb + col][2 * (g * KSG + k) + half]), q[g * KSG + k], z);
-                if constexpr (DYNAMIC) {
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const v4f step = *reinterpret_cast<const v4f*>(&sh.ks[buf][g][32 * tb + 2 * i + 4 * half]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float& to = x[16 * tb + i + j];
-                            to = g == 0 ? z[i + j] * step[j] : fmaf(z[i + j], step[j], to);
-                        }
-                    }
-                    // (computed here, and not sunk to where the scores are used: all groups' products and steps would not fit the registers)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(x[16 * tb + i]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[16 * tb + i] = z[i];
-                }
-            }
-        }
-    };
-    auto multiply = [&](int buf, int first, int count, const v4u (&p)[4]) PQ_INLINE {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int d = first; d < first + count; ++d)
-                o[d] = product(*reinterpret_cast<const v8h*>(&sh.v[buf][k][half][32 * d + col][0]), __builtin_bit_cast(v8h, p[k]), o[d]);
-    };
-
     // ---- the history: wavefronts w and w + 4 load and expand keys and values of tokens 16 w .. 16 w + 15 of every tile
     const int32_t* table = a.table + (int64_t)at.b * a.table_pages;
     const int block = wave & 3;
@@ -335,41 +212,178 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
 
     Codes next;
     int page = 0;
-    if (begin < end) {                             // (on their way while the prefix tokens are taken)
+    if (begin < end) {                             // (on their way while the queries are and the prefix tokens are taken)
         load(begin, page_of(begin), next);
         page = page_of(begin + 1);
     }
 
-    // ---- prefix tokens: as a tile of their own, in fp16
-    if (a.n_prefix > 0 && split == 0) {
-        for (int t0 = 0; t0 < a.n_prefix; t0 += kTile) {
+    // ---- prefix tokens, in tiles of 32: a thread's token and eight channels of it
+    const bool prefix = a.n_prefix > 0 && split == 0;
+    const int prefix_t = tid / (D / 8), prefix_c = tid % (D / 8);
+    v4u prefix_k = {}, prefix_v = {};
+    auto load_prefix = [&](int t0) PQ_INLINE {
+        if (prefix_t >= kPrefixTile) return;
+        const int64_t from = ((int64_t)min(t0 + prefix_t, a.n_prefix - 1) * Hkv + head) * D + 8 * prefix_c;
+        prefix_k = *reinterpret_cast<const v4u*>(a.prefix_k + from);
+        prefix_v = *reinterpret_cast<const v4u*>(a.prefix_v + from);
+    };
+    if (prefix) load_prefix(0);
+
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[s] = in_key_order(__builtin_bit_cast(v4u, q[s]));
+    if constexpr (!DYNAMIC) {
+        const v4u minus8 = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+        v16f z = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) z = product(__builtin_bit_cast(v8h, minus8), q[s], z);
+        c0 = z[0];
+    }
+
+    const float scale = a.softmax_scale * 1.44269504088896341f;
+    float c1 = scale * kUnit, v_step = 1.0f;
+    if constexpr (!DYNAMIC) {
+        c1 *= a.cache.k_scale[head];
+        v_step = a.cache.v_scale[head];
+    }
+
+    float m = kNothing, l = 0.0f;
+    float ref[NG];                           // dynamic steps: weights p * step are rounded relative to ref
+    v16f o[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i] = (v16f){};
+#pragma unroll
+    for (int g = 0; g < NG; ++g) ref[g] = kLeast;
+
+    // exp2(c1 x + bias - m) of a tile's scores.  The reference m follows the largest; what is there is rescaled.
+    auto probabilities = [&](auto& x, float c1, float bias, auto& p) PQ_INLINE {
+        constexpr int N = sizeof(x) / sizeof(x[0]);
+        float most = x[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+        most = fmaf(most, c1, bias);
+        if (__builtin_amdgcn_ballot_w64(most > m + kMost) != 0) {
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const float to_m = most > m + kMost ? ceilf(most) - kBack : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - to_m);
+            m = to_m;
+            l *= alpha;
+            if constexpr (DYNAMIC) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float y = ref[g] * alpha, f = y >= kLeast ? 1.0f : y * (1.0f / kLeast);
+                    ref[g] = fmaxf(y, kLeast);
+#pragma unroll
+                    for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < DB; ++i) o[i] *= alpha;
+            }
+        }
+        const float minus = bias - m;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c1, minus));
+            x[i + 1] = __builtin_amdgcn_exp2f(fmaf(x[i + 1], c1, minus));
+            const uint32_t two = two_halves(x[i], x[i + 1]);
+            p[i >> 3][(i & 7) >> 1] = two;
+            l = add_halves(two, l);
+        }
+    };
+    // dynamic steps: the weights p * step of one group, rounded relative to ref, which moves as m does
+    auto weights = [&](int buf, int g, const float (&x)[32], float most_x, v4u (&p)[4]) PQ_INLINE {
+        const v4f most4 = *reinterpret_cast<const v4f*>(&sh.vs_most[buf][g][0]);
+        const float most_step = fmaxf(fmaxf(most4[0], most4[1]), fmaxf(most4[2], most4[3]));
+        // no weight is larger than this product
+        if (__builtin_amdgcn_ballot_w64(most_x * most_step > 0x1.0p14f * ref[g]) != 0) {
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = fmaxf(most, x[i + j] * step[j]);
+            }
+            most = fmaxf(most, __shfl_xor(most, 32, 64)) * inverse(ref[g]);
+            const int up = most > 0x1.0p14f ? ilogbf(most) - (int)kBack : 0;
+            const float f = ldexpf(1.0f, -up);
+            ref[g] = ldexpf(ref[g], up);
+#pragma unroll
+            for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
+        }
+        const float inv = inverse(ref[g]);
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const v4f step = *reinterpret_cast<const v4f*>(&sh.vs[buf][g][2 * i + 4 * half]);
+            p[i >> 3][(i & 7) >> 1] = two_halves(x[i] * inv * step[0], x[i + 1] * inv * step[1]);
+            p[i >> 3][((i & 7) >> 1) + 1] = two_halves(x[i + 2] * inv * step[2], x[i + 3] * inv * step[3]);
+        }
+    };
+    // scores x of a tile [token 32 tb + 8 (i / 4) + 4 half + i % 4], in units of a code (dynamic: of 2^20 steps)
+    auto scores = [&](int buf, auto& x) PQ_INLINE {
+        constexpr int TB = sizeof(x) / sizeof(x[0]) / 16;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) {
+                v16f z = {};
+#pragma unroll
+                for (int k = 0; k < KSG; ++k)
+                    z = product(__builtin_bit_cast(v8h, sh.k[buf][32 * tb + col][2 * (g * KSG + k) + half]), q[g * KSG + k], z);
+                if constexpr (DYNAMIC) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const v4f step = *reinterpret_cast<const v4f*>(&sh.ks[buf][g][32 * tb + 2 * i + 4 * half]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float& to = x[16 * tb + i + j];
+                            to = g == 0 ? z[i + j] * step[j] : fmaf(z[i + j], step[j], to);
+                        }
+                    }
+                    // (computed here, and not sunk to where the scores are used: all groups' products and steps would not fit the registers)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(x[16 * tb + i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[16 * tb + i] = z[i];
+                }
+            }
+        }
+    };
+    auto multiply = [&](int buf, int first, int count, const auto& p) PQ_INLINE {
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof(p) / sizeof(p[0])); ++k)
+#pragma unroll
+            for (int d = first; d < first + count; ++d)
+                o[d] = product(*reinterpret_cast<const v8h*>(&sh.v[buf][k][half][32 * d + col][0]), __builtin_bit_cast(v8h, p[k]), o[d]);
+    };
+
+    // ---- prefix tokens, in fp16 where the codes' operands lie
+    if (prefix) {
+        for (int t0 = 0; t0 < a.n_prefix; t0 += kPrefixTile) {
             __syncthreads();
-            for (int i = tid; i < kTile * (D / 8); i += kThreads) {
-                const int t = i / (D / 8), c = i % (D / 8);
-                const int64_t from = ((int64_t)min(t0 + t, a.n_prefix - 1) * Hkv + head) * D + 8 * c;
-                sh.k[0][t][c] = __builtin_bit_cast(v4u, in_key_order(*reinterpret_cast<const v4u*>(a.prefix_k + from)));
-                const v4u x = *reinterpret_cast<const v4u*>(a.prefix_v + from);
-                // token t of its 16: 8 (t / 8) + 4 (half of the lanes) + t % 4
-                const int in16 = t & 15;
+            if (prefix_t < kPrefixTile) {
+                const int t = prefix_t, in16 = t & 15;             // token t of its 16: 8 (t / 8) + 4 (half of the lanes) + t % 4
+                sh.k[0][t][prefix_c] = __builtin_bit_cast(v4u, in_key_order(prefix_k));
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    __half* dst = reinterpret_cast<__half*>(&sh.v[0][t >> 4][(in16 >> 2) & 1][place_of<G>(8 * c + j)][in16 >> 3]);
-                    dst[in16 & 3] = reinterpret_cast<const __half*>(&x)[j];
+                    __half* dst = reinterpret_cast<__half*>(&sh.v[0][t >> 4][(in16 >> 2) & 1][place_of<G>(8 * prefix_c + j)][in16 >> 3]);
+                    dst[in16 & 3] = reinterpret_cast<const __half*>(&prefix_v)[j];
                 }
             }
             if constexpr (DYNAMIC) {
-                if (tid < kTile) {
+                if (tid < kPrefixTile) {
 #pragma unroll
                     for (int g = 0; g < NG; ++g) sh.ks[0][g][tid] = 1.0f;
                 }
             }
+            if (t0 + kPrefixTile < a.n_prefix) load_prefix(t0 + kPrefixTile);
             __syncthreads();
-            float x[32];
-            v4u p[4];
+            float x[kPrefixTile / 2];
+            v4u p[kPrefixTile / 16];
             scores(0, x);
             const int left = a.n_prefix - t0 - 4 * half;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < kPrefixTile / 2; ++i)
                 if (8 * (i >> 2) + (i & 3) >= left) x[i] = -INFINITY;
             probabilities(x, scale, 0.0f, p);
             multiply(0, 0, DB, p);
@@ -455,12 +469,33 @@ __global__ __launch_bounds__(kThreads, 2) void k_kv4_attention_tiles(AttentionAr
     __syncthreads();
     __half* const lines = reinterpret_cast<__half*>(raw_lds) + wave * kCols * (D + 8);
     const float f = l_all > 0.0f ? 1.0f / l_all : 0.0f;
+    if constexpr (G >= 64) {                       // a lane holds eight channels in a row, 16 bytes
+        constexpr int kStep = G / 8, kOver = 16 / kStep;           // rows of the accumulators between them, of them in one block
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+        for (int d0 = 0; d0 < DB; d0 += DBG)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            lines[col * (D + 8) + channel_of<G>(32 * d + 8 * (i >> 2) + 4 * half + (i & 3))] =
-                __float2half_rn(fmaf(o[d][i], times[d / DBG], -minus) * f);
+            for (int i0 = 0; i0 < 16 / (2 * kOver); ++i0) {
+                v4u w;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    float y[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int d = d0 + (e + k) / (2 * kOver), i = i0 + (e + k) % (2 * kOver) * (16 / (2 * kOver));
+                        y[k] = fmaf(o[d][i], times[d / DBG], -minus) * f;
+                    }
+                    w[e / 2] = two_halves(y[0], y[1]);
+                }
+                *reinterpret_cast<v4u*>(lines + col * (D + 8) + channel_of<G>(32 * d0 + 8 * (i0 >> 2) + 4 * half + (i0 & 3))) = w;
+            }
+    } else {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                lines[col * (D + 8) + channel_of<G>(32 * d + 8 * (i >> 2) + 4 * half + (i & 3))] =
+                    __float2half_rn(fmaf(o[d][i], times[d / DBG], -minus) * f);
+    }
     // (each wavefront its own rows: what it reads here it has written itself)
     constexpr int kPer = D / 8;                    // lanes to a row
     for (int i = lane / kPer; i < kCols; i += 64 / kPer) {
