@@ -224,6 +224,21 @@ def test_refusals_reach_the_caller(pq, monkeypatch):
         call(pq, d, 5)
 
 
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("q_len", [1, 30, 47, 48, 49, 130])
+def test_one_request_and_any_hint(pq, group, q_len):
+    """One request alone, and with a second one beside it (which may go to another kernel), whatever the caller says of its rows."""
+    check_attention(pq, attention_case([333], [q_len], 8, 2, 128, q_len, group, 16, prefix=35), hints=(q_len, 1, 40, 1000))
+    check_attention(pq, attention_case([100, 333], [3, q_len], 8, 2, 128, q_len + 1, group, 16), hints=(q_len, 1000))
+
+
+@pytest.mark.parametrize("group", [0, 32, 128])
+def test_one_prompt_in_parts(pq, group):
+    """Histories in many parts, some of them empty: a table far longer than the history."""
+    for n in (1, 63, 600, 2100):
+        check_attention(pq, attention_case([n], [min(n, 60)], 4, 1, 128, n, group, 64, W=500, prefix=2), hints=(60,))
+
+
 def test_sizes_of_one(pq):
     """One page, one token, one head; no request; no token."""
     c = attention_case([1], [1], 1, 1, 64, 83, 0, 16)
