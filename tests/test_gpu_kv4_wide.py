@@ -232,6 +232,47 @@ def test_one_request_and_any_hint(pq, group, q_len):
     check_attention(pq, attention_case([100, 333], [3, q_len], 8, 2, 128, q_len + 1, group, 16), hints=(q_len, 1000))
 
 
+# (groups of 4 heads and more than 48 queries: the kernel for many rows)
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompts_over_pages_that_are_none(pq, group, causal):
+    c = attention_case([200, 170, 133], [100, 60, 70], 8, 2, 128, 91, group, 16)
+    c["table"][0, 1], c["table"][0, 3], c["table"][0, 12], c["table"][1, 0], c["table"][2, :9] = -1, 1 << 30, len(c["kc"]), -7, -1
+    spare = next(p for p in range(len(c["kc"])) if p not in c["table"])            # page 0 stands in for those that are none: NaN there too
+    if group:
+        for n in ("kc", "vc", "ks", "vs"):
+            c[n][spare] = c[n][0]
+        c["table"] = np.where(c["table"] == 0, spare, c["table"]).astype(np.int32)
+        c["ks"][0] = c["vs"][0] = np.nan
+    check_attention(pq, c, causal)
+
+
+def test_prompts_of_lengths_out_of_range(pq):
+    c = attention_case([60, 64, 5], [60, 64, 50], 8, 2, 128, 92, ps=16, W=4)
+    c["kv"][:] = [-3, 1 << 30, 5]                                                  # more queries than tokens: the first see nothing
+    c["table"][1] = [0, 1, 2, 3]
+    check_attention(pq, c)
+
+
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_with_a_sharp_softmax_and_long_tails(pq, group, D):
+    if group > D:
+        pytest.skip("a group is no longer than a head")
+    check_attention(pq, attention_case([700, 400], [110, 50], 8, 2, D, 93, group, 64, prefix=2, q_size=60.0))
+    check_attention(pq, attention_case([3000], [50], 8, 2, D, 94, group, 64, q_size=1e-3))
+
+
+@pytest.mark.parametrize("D,group", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("prefix", [0, 40])
+def test_prompts_with_dynamic_steps_over_a_wide_range(pq, D, group, prefix):
+    c = attention_case([400, 150], [60, 55], 8, 2, D, 95, group, 64, prefix=prefix)
+    r = np.random.default_rng(0)
+    live = np.isfinite(c["vs"])
+    c["vs"][live] = (10.0 ** r.uniform(-9, 4, live.sum())).astype(np.float32)
+    check_attention(pq, c)
+
+
 @pytest.mark.parametrize("group", [0, 32, 128])
 def test_one_prompt_in_parts(pq, group):
     """Histories in many parts, some of them empty: a table far longer than the history."""
