@@ -2,7 +2,9 @@
 //
 // The queries of a request that share a key/value head (its tokens times the heads of the group) are the columns of the matrix instructions,
 // 16 or 32 of them (CB blocks of 16), so that up to as many read every code once.  Bound by HBM: 128 bytes of codes for a token and head of
-// 128 channels.
+// 128 channels.  One token each of 64 requests of up to 8192 cached ones, 32 heads on 8: 356 MB in 78 us and 4 for the second kernel, where
+// the same loads without any arithmetic take 76 and a kernel that only reads as many bytes in a row 56.  One request of 1537 tokens: 7 us
+// and 4, all latency.
 //
 // Work is cut over the histories, in units of kTile tokens of one request, head and tile of rows.  All units of the call lie one after another,
 // and every wavefront takes an equal run of them, whatever the requests' lengths are: a run that covers a history whole writes its outputs,
@@ -663,13 +665,13 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
 
 // What a call has at most: histories (of 16 rows), and workgroups with something to do.
 struct Most {
-    int64_t items, groups;
+    int64_t items, units, groups;
 };
 Most at_most(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int64_t capacity, int small_rows)
 {
     const int64_t by_rows = T * (n_heads / n_kv_heads) / 16 + B, by_requests = ((int64_t)small_rows + 15) / 16 * B;
     const int64_t items = (by_rows < by_requests ? by_rows : by_requests) * n_kv_heads, units = items * ((capacity + kTile - 1) / kTile);
-    return {items, (units + kWaves - 1) / kWaves};
+    return {items, units, (units + kWaves - 1) / kWaves};
 }
 
 // Scratch memory: partial sums, two to a wavefront, then the list of histories.
@@ -694,8 +696,12 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
     return hip_status(hipGetLastError());
 }
 
-// Column blocks: one, if it holds every request's rows (max_q is right, or more tiles of rows are taken).
-int blocks_for(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv <= 16 ? 1 : 2; }
+// Column blocks: two where requests have more than 16 rows and the histories of 16 rows are more than 48 units for every wavefront; with less
+// to do, twice the runs of half the work are faster.  One | two, us, 32 heads of 128 on 8: 16 requests of up to 4000 tokens with 32 rows
+// (32000 units) 37 | 39, 64 rows 42 | 47, 128 rows (128000) 60 | 57; 64 requests with 20 rows (up to 128000) 55 | 57, 32 rows 69 | 64,
+// 128 rows 190 | 156; one of 131072 with 48 rows (98000) 77 | 69.  Four groups of dynamic steps would not fit the registers twice (16
+// requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
+int blocks_for(int32_t max_q, int32_t per_kv, int64_t units) { return (int64_t)max_q * per_kv > 16 && units > 48 * kGroups * kWaves ? 2 : 1; }
 
 // Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and this one the others.  This | tile kernel, us,
 // 32 heads of 128 on 8: one request of 33000 tokens with 128 rows 56 | 107, 192 63 | 110, 256 77 | 79; 8 of up to 4000 46 | 63, 52 | 54,
@@ -712,7 +718,7 @@ size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_
     const int small_rows = small_rows_for(max_q, n_heads / n_kv_heads, B);
     if (small_rows == 0) return 0;
     const Most most = at_most(T, B, n_heads, n_kv_heads, capacity, small_rows);
-    return (partial_bytes(most.groups, head_dim, blocks_for(max_q, n_heads / n_kv_heads)) + (size_t)(most.items + 1) * sizeof(Item) + 255) & ~(size_t)255;
+    return (partial_bytes(most.groups, head_dim, blocks_for(max_q, n_heads / n_kv_heads, most.units)) + (size_t)(most.items + 1) * sizeof(Item) + 255) & ~(size_t)255;
 }
 
 template <int CB>
@@ -724,7 +730,7 @@ int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int sma
         return launch<64, 64, true, CB>(a, small_rows, ws, st);
     }
     if (group == 0) return launch<128, 128, false, CB>(a, small_rows, ws, st);
-    if (group == 32) return launch<128, 32, true, CB>(a, small_rows, ws, st);
+    if (group == 32) return launch<128, 32, true, 1>(a, small_rows, ws, st);
     if (group == 64) return launch<128, 64, true, CB>(a, small_rows, ws, st);
     return launch<128, 128, true, CB>(a, small_rows, ws, st);
 }
@@ -746,8 +752,9 @@ int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, in
         float* const partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + rows);
         if (const int rc = launch_attention_tiles(a, head_dim, group, small_rows, partial, st); rc != PQ_OK || small_rows == 0) return rc;
     }
-    return blocks_for(max_q, a.heads_per_kv) == 1 ? launch_rows<1>(a, head_dim, group, small_rows, ws, st)
-                                                  : launch_rows<2>(a, head_dim, group, small_rows, ws, st);
+    const int64_t units = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page, small_rows).units;
+    return blocks_for(max_q, a.heads_per_kv, units) == 1 ? launch_rows<1>(a, head_dim, group, small_rows, ws, st)
+                                                         : launch_rows<2>(a, head_dim, group, small_rows, ws, st);
 }
 
 }  // namespace kv4

@@ -6,7 +6,8 @@
 //     cu_q[b]  = sum of q over the requests before b,
 //     token cu_q[b] + i:  position = offset + kv_b + i,  slot = table[b, (kv_b + i) / ps] * ps + (kv_b + i) % ps  (-1 without a page).
 //
-// A few kilobytes to a few megabytes: what counts is that it is one launch.  Every workgroup sums the requests before its own itself
+// A few kilobytes to a few megabytes: what counts is that it is one launch (3 us for 64 decoded tokens, 7 for 1500 requests with some
+// 150000 tokens, 1.9 MB: two dependent rounds of loads and a launch).  Every workgroup sums the requests before its own itself
 // (two integers of each, from the caches), then places its own kChunk requests by a scan of one wavefront, and its threads walk over
 // those requests' tokens as one sequence.  blockIdx.y divides that sequence: one long prompt is written by many workgroups.
 // No workgroup reads what another writes: pages given out in this call are looked up in the free list, not in the table.

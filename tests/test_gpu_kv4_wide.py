@@ -232,6 +232,25 @@ def test_one_request_and_any_hint(pq, group, q_len):
     check_attention(pq, attention_case([100, 333], [3, q_len], 8, 2, 128, q_len + 1, group, 16), hints=(q_len, 1000))
 
 
+# (a table of half a million tokens, as a server's may be: the kernel for few rows takes 32 of them at once)
+@pytest.mark.parametrize("D,group", [(64, 0), (64, 32), (64, 64), (128, 0), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("case", ["ragged", "prefix", "none", "sharp", "steps"])
+def test_few_rows_under_a_long_table(pq, D, group, case):
+    if case == "steps" and group == 0:
+        pytest.skip("dynamic steps")
+    c = attention_case([300, 133, 0, 64, 31, 1], [9, 48, 2, 20, 0, 1], 4, 1, D, 101, group, 64, W=8192, prefix=37 if case == "prefix" else 0,
+                       q_size=40.0 if case == "sharp" else 1.5)
+    if case == "none":
+        c["table"][0, 1], c["table"][1, 0], c["table"][3, 0] = -1, 1 << 30, len(c["kc"])
+    if case == "steps":
+        r = np.random.default_rng(0)
+        live = np.isfinite(c["vs"])
+        c["vs"][live] = (10.0 ** r.uniform(-9, 3, live.sum())).astype(np.float32)
+    first = check_attention(pq, c)
+    assert np.array_equal(first, check_attention(pq, c))
+    check_attention(pq, c, causal=False)
+
+
 # (groups of 4 heads and more than 48 queries: the kernel for many rows)
 @pytest.mark.parametrize("group", [0, 32, 64, 128])
 @pytest.mark.parametrize("causal", [True, False])
