@@ -12,7 +12,7 @@
 //
 // Bound by HBM: 2 bytes of every channel in, 2 out for queries and half a byte for keys and values (8192 tokens x 48 heads of 128: 180 MB in
 // 46 us, 3.9 TB/s, where a copy of as many bytes takes 35); with norms and dynamic steps by vector instructions as well (2111 tokens x 80
-// heads: 81 MB in 31 us); a step of 64 tokens by its launch and three dependent loads (4.5 us).  A lane holds eight channels
+// heads: 81 MB in 27 us); a step of 64 tokens by its launch and three dependent loads (4.5 us).  A lane holds eight channels
 // (16 bytes), D / 8 lanes a head, a wavefront the same head of 8 or 4 consecutive tokens: one kind of work to a wavefront, the step and
 // the norm's weights are read once, and in a page the tokens of a head lie one after another.  The four wavefronts of a workgroup take
 // four neighbouring heads of these tokens, which share the rows of the table of angles.
@@ -57,10 +57,12 @@ template <int LOG2_D> __device__ __forceinline__ constexpr double inv_sqrt()    
     return LOG2_D == 6 ? 0.125 : 0.08838834764831845;
 }
 
-// In fp32 the Hadamard rotation's values carry the sign of rq::lane_sign, which whoever takes them multiplies in.
+// Everything is linear in the norm's factor, which is left to the caller: v times the return value is what was asked for.  In fp32 the Hadamard
+// rotation's values carry the sign of rq::lane_sign as well, which whoever takes them multiplies in.
 template <typename F, int LOG2_D, bool ROTATE>
-__device__ __forceinline__ void turn(const Lane& c, bool norm, Turn rope, F eps, int lane, F (&v)[8])
+__device__ __forceinline__ F turn(const Lane& c, bool norm, Turn rope, F eps, int lane, F (&v)[8])
 {
+    F scale = 1;
     constexpr int kLaneBits = LOG2_D - 3;
     constexpr bool kExact = std::is_same<F, double>::value;
 #pragma unroll
@@ -71,11 +73,10 @@ __device__ __forceinline__ void turn(const Lane& c, bool norm, Turn rope, F eps,
         for (int i = 0; i < 8; ++i) sum += v[i] * v[i];
         sum = sum_lanes<kLaneBits>(sum);
         const F mean = sum * (F)(1.0 / (1 << LOG2_D)) + eps;
-        F scale;
         if constexpr (kExact) scale = 1.0 / sqrt(mean);
         else scale = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= scale * (F)c.w[i];
+        for (int i = 0; i < 8; ++i) v[i] *= (F)c.w[i];
     }
     if (rope != kNone) {
         F other[8];
@@ -117,6 +118,7 @@ __device__ __forceinline__ void turn(const Lane& c, bool norm, Turn rope, F eps,
             });
         }
     }
+    return scale;
 }
 
 // Codes of eight quotients, and whether one of them is nearer than `near` to a border between two codes.
@@ -178,11 +180,9 @@ __device__ __forceinline__ void append_exact(const AppendArgs& a, Lane& ln, Turn
         for (int i = 0; i < 8; ++i) d[i] = (double)ln.x[i];
     } else {
         if (a.k_weight) halves_to_floats(*reinterpret_cast<const v4i*>(a.k_weight + 8 * c), ln.w);
-        turn<double, LOG2_D, ROTATE>(ln, a.k_weight != nullptr, rope, (double)a.eps, lane, d);
-        if constexpr (ROTATE) {
+        const double scale = turn<double, LOG2_D, ROTATE>(ln, a.k_weight != nullptr, rope, (double)a.eps, lane, d) * (ROTATE ? inv_sqrt<LOG2_D>() : 1.0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] *= inv_sqrt<LOG2_D>();
-        }
+        for (int i = 0; i < 8; ++i) d[i] *= scale;
     }
     float step;
     if constexpr (LOG2_GROUP == 0) {
@@ -203,16 +203,18 @@ __device__ __forceinline__ void append_exact(const AppendArgs& a, Lane& ln, Turn
 // The head vectors of one head of the wavefront's tokens: a query's channels, or the codes of a key or value.  Returns the lanes whose
 // codes the fp32 path cannot decide; their vectors are left to append_exact.
 template <int LOG2_D, int LOG2_GROUP, bool ROTATE>
-__device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, Turn rope, const v4i raw, int head, __half* q_row, int64_t token0, bool live, int lane)
+__device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, Turn rope, const v4i raw, int head, __half* q_row, int64_t token0, bool live, bool first, int lane)
 {
     constexpr int D = 1 << LOG2_D, kLanes = D / 8, kLaneBits = LOG2_D - 3;
     constexpr int kGroupBits = LOG2_GROUP ? LOG2_GROUP - 3 : kLaneBits;
     const int c = lane & (kLanes - 1), Hkv = a.cache.n_kv_heads;
     const bool is_query = head < a.n_heads, is_value = head >= a.n_heads + Hkv;
     const bool norm = !is_value && (is_query ? a.q_weight : a.k_weight) != nullptr;
-    if (norm) halves_to_floats(*reinterpret_cast<const v4i*>((is_query ? a.q_weight : a.k_weight) + 8 * c), ln.w);
+    // (a wavefront's heads ascend: queries, then keys)
+    if (norm && (first || head - kThreads / 64 < a.n_heads != is_query))
+        halves_to_floats(*reinterpret_cast<const v4i*>((is_query ? a.q_weight : a.k_weight) + 8 * c), ln.w);
     halves_to_floats(raw, ln.x);
-    const double unit = ROTATE && !is_value ? inv_sqrt<LOG2_D>() : 1.0;
+    float unit = ROTATE && !is_value ? (float)inv_sqrt<LOG2_D>() : 1.0f;
     const float sign = ROTATE && !is_value ? rq::lane_sign(lane, kLaneBits) : 1.0f;
 
     float v[8];
@@ -220,10 +222,10 @@ __device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, T
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = ln.x[i];
     } else {
-        turn<float, LOG2_D, ROTATE>(ln, norm, rope, a.eps, lane, v);
+        unit *= turn<float, LOG2_D, ROTATE>(ln, norm, rope, a.eps, lane, v);
     }
     if (is_query) {
-        const float m = (float)unit * sign;
+        const float m = unit * sign;
         v4i o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -247,17 +249,17 @@ __device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, T
         step = (float)((double)a.clip * ((double)max_lanes<kGroupBits>(most) * unit) / 7.0);
         if (!(step > 0.0f)) step = 1.0f;
     }
-    const float mult = (float)unit / step * sign;
+    const float mult = unit / step * sign;
     float t8[8], norm2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         t8[i] = v[i] * mult;
         norm2 = fmaf(t8[i], t8[i], norm2);
     }
-    // The multiplier and its product are off by 1.5 * 2^-23 of a quotient, 1.5 * 2^-20 at the end of the range.  Norm, position rotation and
-    // butterflies are orthogonal up to a factor: each rounds by 2^-24 of the vector's length at most and passes on what came before, 11 such
-    // roundings in all, and the norm's factor itself is within 8.5 * 2^-24 of its value (half the 12 roundings of the sum of squares, half
-    // of the mean's, the reciprocal root's 2^-23), 8.5 * 2^-21 at the end of the range: with the first less than 2^-17.
+    // The multiplier and its product are off by 2^-22 of a quotient, 2^-19 at the end of the range.  The norm's weights, position rotation and
+    // butterflies: each rounds by 2^-24 of the vector's length at most and what follows passes it on (the rotations are orthogonal up to a
+    // factor), ten such roundings in all, and the norm's factor itself is within 8.5 * 2^-24 of its value (half the 12 roundings of the sum
+    // of squares, half of the mean's, the reciprocal root's 2^-23), 8.5 * 2^-21 at the end of the range: with the first less than 2^-17.
     float near = 0x1.0p-17f;
     if (!is_value) near += 0x1.0p-20f * __builtin_amdgcn_sqrtf(sum_lanes<kLaneBits>(norm2));
     bool suspect;
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
         }
     }
     if constexpr (!MANY) {
-        const uint64_t found = append_head<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, raw, head, q_row, token0, live, lane);
+        const uint64_t found = append_head<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, raw, head, q_row, token0, live, true, lane);
         if (found != 0) append_exact<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, head, token0, found, lane);
         return;
     }
@@ -338,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
     for (int j = 0;; ++j) {
         const v4i now = raw;
         if (head + kStride < end) raw = load(head + kStride);
-        const uint64_t found = append_head<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, now, head, q_row, token0, live, lane);
+        const uint64_t found = append_head<LOG2_D, LOG2_GROUP, ROTATE>(a, ln, rope, now, head, q_row, token0, live, j == 0, lane);
         if (found != 0) {
             asked |= 1u << j;
             suspects[wave][j] = found;

@@ -138,7 +138,7 @@ def check_append(pq, c, Hq, Hkv, D, group=0, norm=None, cos_sin=None, interleave
             step = R.steps_of(y, group, clip)
             stored = host(scales)[page, :, at]
             # Both sides round to fp32.  A key's channels come out of the fp32 path with at most 12 roundings of 2^-24 of the vector's length
-            # (two products of the norm, two of the position rotation, seven butterflies, one multiplier), and the norm's factor, common to
+            # (the norm's weight, two of the position rotation, seven butterflies, two of the multiplier), and the norm's factor, common to
             # all, with half of the 12 of its sum of squares, half of one for the mean, 2^-23 of the reciprocal root: 8.5 * 2^-24.  The
             # largest moves by no more than that, and the step by clip / 7 of it.
             off = 2.0 ** -23 * step
