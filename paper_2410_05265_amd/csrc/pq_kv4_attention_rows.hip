@@ -98,11 +98,11 @@ struct Item {
 // 16 or 4 bytes of every lane from memory straight into LDS, lane after lane from lds_addr (wavefront-uniform) on.
 __device__ __forceinline__ void to_lds16(const void* src, uint32_t lds_addr)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_addr) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds_addr)) : "memory");
 }
 __device__ __forceinline__ void to_lds4(const void* src, uint32_t lds_addr)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds_addr) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds_addr)) : "memory");
 }
 
 template <int D, int G, bool DYNAMIC, int CB>
