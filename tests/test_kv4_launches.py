@@ -47,7 +47,7 @@ def test_attention_takes_what_its_rules_say():
     assert kernels(attention(T=256, max_q=4)) == one                                # 16 rows
     assert kernels(attention(T=320, max_q=5)) == two                                # more, and 160 units and more for every wavefront
     assert kernels(attention(T=40, B=8, max_q=5)) == one                            # little to read
-    assert kernels(attention(T=64 * 48, max_q=48)) == two                           # 192 rows
+    assert kernels(attention(T=60 * 48, B=60, max_q=48)) == two                         # 192 rows
     assert kernels(attention(T=64 * 49, max_q=49)) == [tiles] + two                 # more: the tile kernel for those that have them
     assert kernels(attention(T=400, B=8, max_q=300, W=1)) == [tiles] + one
     assert kernels(attention(T=4096, B=1, max_q=4096, W=64)) == [tiles]             # a single request
