@@ -2,9 +2,8 @@
 //
 // The queries of a request that share a key/value head (its tokens times the heads of the group) are the columns of the matrix instructions,
 // 16 or 32 of them (CB blocks of 16), so that up to as many read every code once.  Bound by HBM: 128 bytes of codes for a token and head of
-// 128 channels.  One token each of 64 requests of up to 8192 cached ones, 32 heads on 8: 356 MB in 78 us and 4 for the second kernel, where
-// the same loads without any arithmetic take 76 and a kernel that only reads as many bytes in a row 56.  One request of 1537 tokens: 7 us
-// and 4, all latency.
+// 128 channels.  One token each of 64 requests of up to 8192 cached ones, 32 heads on 8: 356 MB in 70 us and 4 for the second kernel, where
+// a kernel that only reads as many bytes in a row takes 56.  One request of 1537 tokens: 7 us and 4, all latency.
 //
 // Work is cut over the histories, in units of kTile tokens of one request, head and tile of rows.  All units of the call lie one after another,
 // and every wavefront takes an equal run of them, whatever the requests' lengths are: a run that covers a history whole writes its outputs,
@@ -95,7 +94,11 @@ struct Item {
     int worker, parts, second, start, rows, head, row0, unused;
 };
 
-// 16 or 4 bytes of every lane from memory straight into LDS, lane after lane from lds_addr (wavefront-uniform) on.
+// 16 or 4 bytes of every lane from memory straight into LDS, lane after lane from lds_addr (wavefront-uniform) on; `once`: past the caches.
+__device__ __forceinline__ void to_lds16_once(const void* src, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds_addr)) : "memory");
+}
 __device__ __forceinline__ void to_lds16(const void* src, uint32_t lds_addr)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds_addr)) : "memory");
@@ -127,6 +130,10 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
     const uint32_t ring_addr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)ring;
 
     const Plan p = plan<ROWS>(a, small_rows, lane);
+    // Codes that one wavefront reads once go past the caches, where they would push out each other and, from call to call, themselves: a call's
+    // history from 64 MiB on (356 MB 82 -> 73.5 us, 148 MB 43.2 -> 39.8, 342 MB with dynamic steps 84.5 -> 79.9); below, they may be in the
+    // memory-side cache still (27 MB read by each of three calls in turn: 23.4 -> 24.6).
+    const bool stream = p.total * (2 * S::CODES) > 64 << 20;
     // (place 0 holds their count; only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
     if (blockIdx.x == 0 && threadIdx.x == 0) items[0].parts = (int)min(p.items, most_items);
     // the first `more` runs have one unit more
@@ -208,17 +215,21 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                 first[blk] = (((int64_t)(bad ? 0 : page) * Hkv + head) << log2_page) + (t & ((1 << log2_page) - 1));
             }
             const uint32_t to_addr = ring_addr + place * S::SLOT;
-            if constexpr (D == 128) {
+            auto codes = [&](auto to_lds) PQ_INLINE {
+                if constexpr (D == 128) {
 #pragma unroll
-                for (int blk = 0; blk < 2; ++blk) {
-                    to_lds16(a.cache.k_codes + first[blk] * 64 + 16 * lane, to_addr + 1024 * blk);
-                    to_lds16(a.cache.v_codes + first[blk] * 64 + 16 * lane, to_addr + S::CODES + 1024 * blk);
+                    for (int blk = 0; blk < 2; ++blk) {
+                        to_lds(a.cache.k_codes + first[blk] * 64 + 16 * lane, to_addr + 1024 * blk);
+                        to_lds(a.cache.v_codes + first[blk] * 64 + 16 * lane, to_addr + S::CODES + 1024 * blk);
+                    }
+                } else {                           // 32 lanes to a block
+                    const int64_t at = (lane < 32 ? first[0] : first[1]) * 32 + 16 * (lane & 31);
+                    to_lds(a.cache.k_codes + at, to_addr);
+                    to_lds(a.cache.v_codes + at, to_addr + S::CODES);
                 }
-            } else {                               // 32 lanes to a block
-                const int64_t at = (lane < 32 ? first[0] : first[1]) * 32 + 16 * (lane & 31);
-                to_lds16(a.cache.k_codes + at, to_addr);
-                to_lds16(a.cache.v_codes + at, to_addr + S::CODES);
-            }
+            };
+            if (stream && tiles == 1) codes([](const void* src, uint32_t to) PQ_INLINE { to_lds16_once(src, to); });
+            else codes([](const void* src, uint32_t to) PQ_INLINE { to_lds16(src, to); });
             if constexpr (DYNAMIC) {
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {     // step e of the tile's 32 NG: token e / NG, group e % NG

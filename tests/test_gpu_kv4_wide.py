@@ -108,6 +108,18 @@ def test_attention_more_histories_than_workgroups(pq):
         assert np.all(np.abs(got[b0:b0 + n] - o) <= bound)
 
 
+@pytest.mark.parametrize("D,Hkv,group", [(128, 2, 0), (128, 2, 64), (64, 4, 32)])
+def test_attention_streams_large_caches(pq, D, Hkv, group):
+    """More than 64 MiB of codes in a call, which go past the caches: one token each of nine requests, one of them with more rows than a
+    wavefront takes (its codes are read twice)."""
+    c = attention_case([33500] * 8 + [5000], [1] * 8 + [20], Hkv, Hkv, D, 111, group, 128, prefix=2)
+    d = put(c)
+    assert sum(int(n) for n in c["kv"]) * Hkv * D > 64 << 20
+    got = [host(call(pq, d, 20)) for _ in range(2)]
+    assert np.array_equal(got[0], got[1])
+    within(c, got[0])
+
+
 # ------------------------------------------------------------------------------------------------ past 32 bits
 @pytest.mark.parametrize("group", [0, 64])
 def test_caches_past_32_bits(pq, group):
