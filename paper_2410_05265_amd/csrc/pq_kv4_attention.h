@@ -14,7 +14,10 @@
 //
 // Probabilities are rounded to fp16 relative to a reference m that lags behind the running maximum: it moves only when a score passes it by
 // 14 (p <= 2^14), and then to 6 above which 2^6 = p stands.  p keeps fp16's full precision down to 2^-20 of the largest, the accumulators are
-// rescaled only when the reference moves, by a power of two, and the denominator sums what was rounded.
+// rescaled only when the reference moves, by a power of two, and the denominator sums what was rounded: where one token has all the weight its
+// rounding leaves again.  With dynamic steps the product takes weights p * step, rounded once, a rounding for every group of channels; the
+// denominator then sums p as it is: the sum of rounded p would be a second, independent error, sqrt(3) instead of sqrt(2) times the rounding of
+// the fp16 result where one token has the weight (measured over histories of 1 to 2000 tokens: 1.40 to 1.45, static steps 1.0 to 1.44).
 #pragma once
 
 #include "pq_kv4.h"

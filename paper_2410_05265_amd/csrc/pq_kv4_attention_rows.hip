@@ -325,7 +325,8 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 pr[i] = two_halves(x[2 * i], x[2 * i + 1]);
-                l[c] = add_halves(pr[i], l[c]);
+                if constexpr (DYNAMIC) l[c] += x[2 * i] + x[2 * i + 1];    // (the product rounds weights, and not these)
+                else l[c] = add_halves(pr[i], l[c]);
             }
         };
 

@@ -293,7 +293,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             x[i + 1] = __builtin_amdgcn_exp2f(fmaf(x[i + 1], c1, minus));
             const uint32_t two = two_halves(x[i], x[i + 1]);
             p[i >> 3][(i & 7) >> 1] = two;
-            l = add_halves(two, l);
+            if constexpr (DYNAMIC) l += x[i] + x[i + 1];           // (the product rounds weights, and not these)
+            else l = add_halves(two, l);
         }
     };
     // dynamic steps: the weights p * step of one group, rounded relative to ref, which moves as m does
