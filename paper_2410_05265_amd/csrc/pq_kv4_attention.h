@@ -75,6 +75,10 @@ __device__ __forceinline__ float add_halves(uint32_t pair, float to)
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, pair), one, to, false);
 }
 
+// A value's dynamic step, times a probability of zero, is zero: one that is not finite (of a token with an infinite value) counts as the
+// largest number, so that who sees the token leaves fp16's range, and who does not is not touched.
+__device__ __forceinline__ float finite_step(float s) { return fmaxf(fminf(s, __FLT_MAX__), 0.0f); }
+
 // 1 / x of a power of two.
 __device__ __forceinline__ float inverse(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
 

@@ -499,8 +499,9 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                     for (int j = 0; j < 8; ++j) {
                         const int e = (j & 3) * NG + g;
                         step[j] = vs[j >> 2][e / 4][e % 4];
-                        // what lies behind the last token may be anything: it must not meet a probability of zero
-                        if (masked && (16 * (j >> 2) + (j & 3) >= left || (j < 4 ? bad0 : bad1))) step[j] = 0.0f;
+                        // what lies behind the last token may be anything, and what only later queries see may be infinite: neither must
+                        // meet a probability of zero as it is
+                        if (masked) step[j] = 16 * (j >> 2) + (j & 3) >= left || (j < 4 ? bad0 : bad1) ? 0.0f : finite_step(step[j]);
                     }
 #pragma unroll
                     for (int c = 0; c < CB; ++c) {

@@ -205,8 +205,9 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
                 sh.v[buf][block][quad & 1][place_of<G>(D / 16 * c + j)][quad >> 1] = DYNAMIC ? without_offset<4>(y) : y;
             });
             if constexpr (DYNAMIC) {
-                // what lies behind the last token, or in no page, may be anything: it must not meet a probability of zero
-                const float step = tile * kTile + t < r.n && !x.bad ? x.s : 0.0f;
+                // what lies behind the last token, or in no page, may be anything, and what only later queries see may be infinite: neither
+                // must meet a probability of zero as it is
+                const float step = tile * kTile + t < r.n && !x.bad ? finite_step(x.s) : 0.0f;
                 float most = step;
 #pragma unroll
                 for (int d = 4; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
