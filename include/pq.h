@@ -597,7 +597,9 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
  * query head h reads key/value head h / (n_heads / n_kv_heads).  Keys and values are code * step.  A query that sees nothing gets zeros.
  * q_f16     in  [T, n_heads * head_dim] fp16, rows row_stride values apart (a multiple of 8).
  * cu_q      in  int32 [B + 1], ascending;  kv_len: int32 [B], the new tokens included;  block_table: int32 [B, table_pages].
- *               kv_len is cut off at the table's pages; tokens of entries outside [0, n_pages) count as not seen.
+ *               Tokens behind the table's pages, and of entries outside [0, n_pages), count as not seen; a kv_len that is no length counts as 0
+ *               (negative) or as the table's tokens (2^30 and more, longer than any table).  Rows past T (a step with more new tokens
+ *               than rows) do not exist: the others see what they would see beside them.
  * max_q     the most queries of a request: (>= 1) a hint that chooses between kernels: any value is right, and changes results in the order of sums alone.
  * prefix_k, prefix_v  in fp16 [n_prefix, n_kv_heads, head_dim] (rotated like the keys), NULL iff n_prefix = 0; n_prefix <= 1024.
  * out_f16   out [T, n_heads * head_dim] fp16; rows outside [cu_q[0], cu_q[B]) are left as they were; may not lie over q.

@@ -82,19 +82,32 @@ __device__ __forceinline__ float finite_step(float s) { return fmaxf(fminf(s, __
 // 1 / x of a power of two.
 __device__ __forceinline__ float inverse(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
 
-// A request as the kernels see it: nothing that lies on the device takes them out of bounds.
+// A request as the kernels see it: nothing that lies on the device takes them out of bounds.  Its rows may end with the call's (T), its history
+// with the table; what a row sees is counted from the whole lengths all the same.
 struct Request {
-    int32_t start, q_len, n;     // first row, rows, cached tokens
+    int32_t start, q_len, n;     // first row, rows, cached tokens within the table
+    int32_t sees;                // causal: tokens that the first row sees, of any number (may be negative); a later one as many more
 };
 
+constexpr int64_t kMostTokens = 1 << 30;                   // (no table is that long)
 __device__ __forceinline__ Request request(const AttentionArgs& a, int b)
 {
     Request r;
-    const int64_t from = min(max((int64_t)a.cu_q[b], (int64_t)0), a.T), to = min(max((int64_t)a.cu_q[b + 1], from), a.T);
+    const int64_t begin = a.cu_q[b], end = max((int64_t)a.cu_q[b + 1], begin);
+    const int64_t from = min(max(begin, (int64_t)0), a.T), to = min(max(end, from), a.T), capacity = (int64_t)a.table_pages << a.cache.log2_page;
+    int64_t kv = max(a.kv_len[b], 0);
+    if (kv >= kMostTokens) kv = capacity;                  // (no length: as many as there may be)
     r.start = (int32_t)from;
     r.q_len = (int32_t)(to - from);
-    r.n = (int32_t)min((int64_t)max(a.kv_len[b], 0), (int64_t)a.table_pages << a.cache.log2_page);
+    r.n = (int32_t)min(kv, capacity);
+    r.sees = (int32_t)min(max(kv - (end - 1 - from), -kMostTokens), kMostTokens);
     return r;
+}
+
+// Tokens that row `token` of a request sees, and those that every row from it on sees.
+__device__ __forceinline__ int sees(const AttentionArgs& a, const Request& r, int token)
+{
+    return a.causal ? min(max(r.sees + token, 0), r.n) : r.n;
 }
 
 // Requests of more than small_rows rows (tokens times query heads of a key/value head); the others are the row kernel's.

@@ -64,7 +64,7 @@ __device__ __forceinline__ Plan plan(const AttentionArgs& a, int small_rows, int
     p.first = min(lane * each, a.B);
     p.last = min(p.first + each, a.B);
     p.own = 0;
-    p.r = {0, 0, 0};
+    p.r = {0, 0, 0, 0};
     int64_t items = 0;
     for (int b = p.first; b < p.last; ++b) {
         p.r = request(a, b);
@@ -171,6 +171,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         r.start = __builtin_amdgcn_readfirstlane(__shfl(r.start, from, 64));
         r.q_len = __builtin_amdgcn_readfirstlane(__shfl(r.q_len, from, 64));
         r.n = __builtin_amdgcn_readfirstlane(__shfl(r.n, from, 64));
+        r.sees = __builtin_amdgcn_readfirstlane(__shfl(r.sees, from, 64));
     }
 
     for (int64_t u0 = range; u0 < range_end;) {
@@ -186,9 +187,8 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         const int head = __builtin_amdgcn_readfirstlane((int)item / tiles), tile = __builtin_amdgcn_readfirstlane((int)item % tiles);
         const int rows = r.q_len * per_kv;
         const int first_token = tile * ROWS / per_kv, last_token = min((tile * ROWS + ROWS - 1) / per_kv, r.q_len - 1);
-        const int all_see = a.causal ? r.n - (r.q_len - 1 - first_token) : r.n;         // tokens before this one need no mask
-        const int any_sees = a.causal ? r.n - (r.q_len - 1 - last_token) : r.n;
-        const int from = (int)(from_unit * kTile), to = (int)min((from_unit + take) * kTile, (int64_t)max(any_sees, 0));
+        const int all_see = sees(a, r, first_token), any_sees = sees(a, r, last_token); // tokens before all_see need no mask
+        const int from = (int)(from_unit * kTile), to = (int)min((from_unit + take) * kTile, (int64_t)any_sees);
         if (from_unit == 0 && lane == 0 && item_base + item < most_items)
             items[1 + item_base + item] = {worker, take == per ? 1 : (int)worker_of(u0 + per - 1) - worker + 1, u0 == range ? 0 : 1, r.start, rows, head,
                                            tile * ROWS, 0};
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             const int row = min(tile * ROWS + 16 * c + col, rows - 1), token = row / per_kv, q_head = head * per_kv + row % per_kv;
-            limit[c] = a.causal ? max(r.n - (r.q_len - 1 - token), 0) : r.n;
+            limit[c] = sees(a, r, token);
             const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
             for (int i = 0; i < NG * KS; ++i) raw[c][i] = *reinterpret_cast<const v4u*>(src + i / KS * G + quarter * (G / 4) + 8 * (i % KS));

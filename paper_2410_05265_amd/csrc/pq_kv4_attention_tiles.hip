@@ -45,7 +45,7 @@ __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r
 __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index, int small_rows, int lane)
 {
     const int each = (a.B + 63) / 64, first = min(lane * each, a.B), last = min(first + each, a.B);
-    Request r = {0, 0, 0};                         // the last of this lane's; up to 64 requests are read once
+    Request r = {0, 0, 0, 0};                       // the last of this lane's; up to 64 requests are read once
     int64_t own = 0;
     for (int b = first; b < last; ++b) {
         r = request(a, b);
@@ -75,7 +75,7 @@ __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index
     }
     const int from = __builtin_ctzll(found);
     auto lanes = [&](int v) PQ_INLINE { return __builtin_amdgcn_readlane(v, from); };
-    return {lanes(b), lanes(tile), {lanes(r.start), lanes(r.q_len), lanes(r.n)}};
+    return {lanes(b), lanes(tile), {lanes(r.start), lanes(r.q_len), lanes(r.n), lanes(r.sees)}};
 }
 
 // Row `at` of the accumulators as a channel: channels of a group lie so in LDS that neighbouring threads of the expansion write
@@ -129,19 +129,19 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     const Request r = at.r;
     const int rows = r.q_len * per_kv, row0 = at.tile * kRows;
     const int last_token = min((row0 + kRows - 1) / per_kv, r.q_len - 1);
-    const int visible = max(a.causal ? r.n - (r.q_len - 1 - last_token) : r.n, 0);
+    const int visible = sees(a, r, last_token);
     const int all_tiles = (visible + kTile - 1) / kTile;
     const int begin = (int)((int64_t)all_tiles * split / splits), end = (int)((int64_t)all_tiles * (split + 1) / splits);
 
     // this lane's query
-    int limit, wave_sees = r.n;              // tokens that it sees, and that all of the wavefront's see
+    int limit, wave_sees;                    // tokens that it sees, and that all of the wavefront's see
     v8h q[KS];
     float c0 = 0.0f;                         // -8 sum(q): the codes' offset (dynamic steps: the operands are without it)
     {
         const int row = min(row0 + wave * kCols + col, rows - 1);
         const int token = row / per_kv, q_head = head * per_kv + row % per_kv;
-        limit = a.causal ? max(r.n - (r.q_len - 1 - token), 0) : r.n;
-        if (a.causal) wave_sees = r.n - (r.q_len - 1 - min(row0 + wave * kCols, rows - 1) / per_kv);
+        limit = sees(a, r, token);
+        wave_sees = sees(a, r, min(row0 + wave * kCols, rows - 1) / per_kv);
         const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h*>(src + 16 * s + 8 * half);

@@ -2,10 +2,11 @@
 
 import numpy as np
 import pytest
+import torch
 
 import kv4_reference as R
-from pq_testlib import host
-from test_gpu_kv4 import attention_case, call, pq, put                                          # noqa: F401 (pq: a fixture)
+from pq_testlib import dev, host
+from test_gpu_kv4 import attention_case, call, i32, pq, put, rope_table                         # noqa: F401 (pq: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +31,78 @@ def test_steps_that_are_not_finite_stay_with_who_sees_them(pq, D, group, q_lens,
     for hint in (1, max(q_lens), 1000):
         got = host(call(pq, put(c), hint)).astype(np.float64).reshape(want.shape)
         assert np.all((np.abs(got - want) <= bound)[clean])
+
+
+# ------------------------------------------------------------------------------------------------ steps that are cut off
+def check_cut(pq, c, T=None, W=None, hints=(1,), causal=True):
+    """The first T rows of case c over the first W pages of its table, against the whole case whose table's other entries are none."""
+    T, W = T or len(c["q"]), W or c["table"].shape[1]
+    whole = dict(c, table=c["table"].copy())
+    whole["table"][:, W:] = -1
+    want, bound, real = R.attention(whole["q"], c["cu"], c["kv"], whole["table"], c["kc"], c["vc"], c["ks"], c["vs"], c["scale"], c["group"],
+                                    c["pk"], c["pv"], causal)
+    d = put(dict(c, q=c["q"][:T].copy(), table=c["table"][:, :W].copy()))
+    for hint in hints:
+        got = host(call(pq, d, hint, causal)).astype(np.float64).reshape(want[:T].shape)
+        err = (np.abs(got - want[:T]) / np.maximum(bound[:T], 1e-30))[real[:T]]
+        assert err.max(initial=0.0) <= 1.0, "hint %d: error is %.3g times its bound" % (hint, err.max())
+
+
+def not_appended(c, T):
+    """The tokens of rows from T on have never been written: their steps may be anything."""
+    if not c["group"]:
+        return c
+    ps = c["kc"].shape[2]
+    for b in range(len(c["kv"])):
+        for t in range(max(T, int(c["cu"][b])), int(c["cu"][b + 1])):
+            at = int(c["kv"][b]) - (int(c["cu"][b + 1]) - t)
+            for n in ("ks", "vs"):
+                c[n][c["table"][b, at // ps], :, at % ps] = (np.nan, np.inf)[t % 2]
+    return c
+
+
+@pytest.mark.parametrize("D,group", [(128, 0), (64, 0), (64, 32), (128, 32), (128, 128)])
+@pytest.mark.parametrize("kv,q_lens,T", [([10], [10], 6), ([300], [200], 130), ([70, 90, 33], [20, 60, 5], 50), ([300, 200, 40], [150, 170, 9], 200),
+                                         ([50, 60, 70], [1, 2, 3], 2), ([333, 333], [130, 200], 131)])
+def test_fewer_rows_than_new_tokens(pq, D, group, kv, q_lens, T):
+    """pq_kv4_slots gives lengths that count every new token; what the rows there are see does not depend on those that are not there."""
+    c = not_appended(attention_case(kv, q_lens, 8, 2, D, T, group, 16, prefix=2), T)
+    check_cut(pq, c, T, hints=(1, max(q_lens), 1000))
+
+
+@pytest.mark.parametrize("D,group", [(128, 0), (64, 32), (128, 128)])
+@pytest.mark.parametrize("kv,q_lens,W", [([100], [50], 4), ([100, 64, 65, 300], [50, 40, 3, 100], 4), ([500, 400], [200, 130], 20), ([90, 20], [1, 1], 2)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_histories_past_the_table(pq, D, group, kv, q_lens, W, causal):
+    """Tokens behind the table's pages are not seen; what the others see stays."""
+    check_cut(pq, attention_case(kv, q_lens, 8, 2, D, W, group, 16), W=W, hints=(1, max(q_lens), 1000), causal=causal)
+
+
+@pytest.mark.parametrize("group,T,W", [(0, 60, 12), (128, 60, 12), (0, 300, 5), (64, 200, 6), (0, 20, 4)])
+def test_a_step_with_too_few_rows_or_pages(pq, group, T, W):
+    """slots, append and attention: more new tokens than rows, more tokens than the table holds."""
+    Hq, Hkv, D, ps, q_lens = 8, 2, 128, 16, [30, 100, 0, 70]
+    r = np.random.default_rng(T)
+    B, pages = len(q_lens), 60
+    kv = np.array([5, 0, 20, 17], np.int32)
+    shape = (pages, Hkv, ps)
+    kc, vc = (r.integers(0, 256, shape + (D // 2,)).astype(np.uint8) for _ in range(2))
+    ks, vs = (r.uniform(0.2, 0.6, shape + (D // group,) if group else (Hkv,)).astype(np.float32) for _ in range(2))
+    table = np.full((B, W), -1, np.int32)
+    order = r.permutation(pages).astype(np.int32)
+    for b in range(B):
+        table[b, :-(-int(kv[b]) // ps)] = order[2 * b:2 * b + -(-int(kv[b]) // ps)]
+    t, kc, vc, ks, vs = dev(table), dev(kc), dev(vc), dev(ks), dev(vs)
+    cu, kv_all, pos, slot, _ = pq.pq_kv4_slots(dev(kv), i32(q_lens), t, dev(order[2 * B:]), ps, T, position_offset=1)
+    qkv = dev(r.standard_normal((T, (Hq + 2 * Hkv) * D)).astype(np.float16))
+    q = torch.zeros((T, Hq * D), dtype=torch.float16, device="cuda")
+    pq.pq_kv4_append(qkv, Hq, pos, slot, kc, vc, ks, vs, cos_sin=dev(rope_table(D)), group=group, out=q)
+    out, _ = pq.pq_kv4_attention(q, cu, kv_all, t, kc, vc, ks, vs, D ** -0.5, max(q_lens), group=group)
+    rows = max(T, sum(q_lens))
+    whole = np.zeros((rows, Hq * D), np.float16)
+    whole[:T] = host(q)
+    wide = np.full((B, 40), -1, np.int32)
+    wide[:, :W] = host(t)
+    want, bound, real = R.attention(whole, host(cu), host(kv_all), wide, host(kc), host(vc), host(ks), host(vs), D ** -0.5, group)
+    got = host(out).astype(np.float64).reshape(want[:T].shape)
+    assert np.all((np.abs(got - want[:T]) <= bound[:T])[real[:T]])
