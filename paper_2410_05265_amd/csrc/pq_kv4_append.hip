@@ -44,8 +44,9 @@ template <int BITS, typename F> __device__ __forceinline__ F max_lanes(F v)
 struct Lane {
     float x[8];
     float w[8];           // the norm's weight, or 1
-    float cs[8], sn[8];   // cosine and sine of each channel's angle, the sine with the sign it enters with; 1 and 0 where nothing turns
+    float cs[8], sn[8];   // cosine and sine of each channel's angle, the sine with the sign it enters with
     int partner;          // lane whose channels turn with this one's (halves of less than a head)
+    bool turns;           // whether these channels turn
 };
 
 // Which channels turn together: none; neighbours; those half a head apart, in lanes one bit apart; those half of rotary_dim apart.
@@ -91,7 +92,10 @@ __device__ __forceinline__ F turn(const Lane& c, bool norm, Turn rope, F eps, in
             for (int i = 0; i < 8; ++i) other[i] = v[i ^ 1];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] * (F)c.cs[i] + other[i] * (F)c.sn[i];
+        for (int i = 0; i < 8; ++i) {
+            const F turned = v[i] * (F)c.cs[i] + other[i] * (F)c.sn[i];
+            v[i] = c.turns ? turned : v[i];        // (not by a sine of zero: an infinity would reach its neighbour)
+        }
     }
     if constexpr (ROTATE) {
         if constexpr (!kExact) {
@@ -129,7 +133,7 @@ __device__ __forceinline__ uint32_t codes8(const float (&t)[8], float near, bool
 #pragma unroll
     for (int i = 7; i >= 0; --i) {
         const float c = __builtin_amdgcn_fmed3f(t[i], -8.0f, 7.0f), r = c + rq::kMagic;
-        suspect |= fabsf(c - (r - rq::kMagic)) > 0.5f - near;
+        suspect |= !(fabsf(c - (r - rq::kMagic)) <= 0.5f - near);     // (no bound, from a NaN in the vector: all of it)
         s = (s << 4) + __float_as_uint(r);
     }
     return (s - rq::kMagicSum) ^ 0x88888888u;
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
         const int half = a.rotary_dim / 2;
         const int64_t position = min(max((int64_t)a.positions[row], (int64_t)0), a.max_positions - 1);
         const float* cs = a.cos_sin + position * a.rotary_dim;
-        const bool turns = 8 * c < a.rotary_dim;
+        const bool turns = ln.turns = 8 * c < a.rotary_dim;
         ln.partner = lane;
         if (a.interleaved) {
             rope = kPairs;
@@ -307,9 +311,9 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
             const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                ln.cs[2 * i] = ln.cs[2 * i + 1] = turns ? xs[i] : 1.0f;
-                ln.sn[2 * i] = turns ? -ys[i] : 0.0f;
-                ln.sn[2 * i + 1] = turns ? ys[i] : 0.0f;
+                ln.cs[2 * i] = ln.cs[2 * i + 1] = xs[i];
+                ln.sn[2 * i] = -ys[i];
+                ln.sn[2 * i + 1] = ys[i];
             }
         } else {
             rope = a.rotary_dim == D ? kHalfHead : kHalves;
@@ -322,8 +326,8 @@ __global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
                 const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    ln.cs[i + k] = turns ? xs[k] : 1.0f;
-                    ln.sn[i + k] = turns ? (first ? -ys[k] : ys[k]) : 0.0f;
+                    ln.cs[i + k] = xs[k];
+                    ln.sn[i + k] = first ? -ys[k] : ys[k];
                 }
             }
         }

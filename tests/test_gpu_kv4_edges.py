@@ -6,7 +6,7 @@ import torch
 
 import kv4_reference as R
 from pq_testlib import dev, host
-from test_gpu_kv4 import attention_case, call, i32, pq, put, rope_table                         # noqa: F401 (pq: a fixture)
+from test_gpu_kv4 import append_case, attention_case, call, i32, pq, put, rope_table            # noqa: F401 (pq: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -31,6 +31,38 @@ def test_steps_that_are_not_finite_stay_with_who_sees_them(pq, D, group, q_lens,
     for hint in (1, max(q_lens), 1000):
         got = host(call(pq, put(c), hint)).astype(np.float64).reshape(want.shape)
         assert np.all((np.abs(got - want) <= bound)[clean])
+
+
+@pytest.mark.parametrize("D,rd", [(128, 64), (128, 96), (64, 16), (128, 0)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T", [40, 2400])                          # (a head to a wavefront, and several)
+def test_append_infinities_stay_in_their_channel(pq, D, rd, interleaved, T):
+    """Channels that do not turn are what they were, whatever their neighbours hold; some vectors take the 64-bit path."""
+    Hq, Hkv = 22, 11
+    c = append_case(T, Hq, Hkv, D, T + rd, 0)
+    r = np.random.default_rng(rd)
+    c["ks"][:], c["vs"][:] = 0.25, 0.125
+    x = c["qkv"].reshape(T, Hq + 2 * Hkv, D)
+    odd = r.random((T, Hq + 2 * Hkv)) < 0.5
+    x[odd, rd + 1] = np.float16(0.375)                             # on a border of the keys' codes (1.5 steps) and of the values' (3)
+    for what in (np.inf, -np.inf, np.nan):
+        at = r.integers(rd, D, (T, Hq + 2 * Hkv))
+        put_here = r.random((T, Hq + 2 * Hkv)) < 0.3
+        t, h = np.nonzero(put_here)
+        x[t, h, at[t, h]] = what
+    assert np.isfinite(x[..., :rd]).all()
+    z = R.turn(x[:, :Hq + Hkv], None, 0, rope_table(rd) if rd else None, c["positions"], interleaved, False)
+    t = [dev(c[n]) for n in ("kc", "vc", "ks", "vs")]
+    q = host(pq.pq_kv4_append(dev(c["qkv"]), Hq, dev(c["positions"]), dev(c["slots"]), *t, cos_sin=dev(rope_table(rd)) if rd else None,
+                              interleaved=interleaved, rotate=False)).astype(np.float64).reshape(T, Hq, D)
+    assert np.array_equal(q[..., rd:], z[:, :Hq, rd:], equal_nan=True)                   # as they came
+    assert np.all(np.abs(q[..., :rd] - z[:, :Hq, :rd]) <= 2.0 ** -11 * np.abs(z[:, :Hq, :rd]) + 2.0 ** -20 * 64)   # (pairs no longer than 64)
+    page, at = c["slots"] // 16, c["slots"] % 16
+    for codes, y, step in ((t[0], z[:, Hq:], c["ks"]), (t[1], x[:, Hq + Hkv:].astype(np.float64), c["vs"])):
+        number = ~np.isnan(y)                                      # (a NaN has no code)
+        want = R.codes_of(np.where(number, y, 0), step[None, :, None])
+        got = R.unpack(host(codes)[page, :, at])
+        assert np.array_equal(got[number], want[number])
 
 
 # ------------------------------------------------------------------------------------------------ steps that are cut off
