@@ -8,8 +8,10 @@
 //
 // A few kilobytes to a few megabytes: what counts is that it is one launch (3 us for 64 decoded tokens, 7 for 1500 requests with some
 // 150000 tokens, 1.9 MB: two dependent rounds of loads and a launch).  Every workgroup sums the requests before its own itself
-// (two integers of each, from the caches), then places its own kChunk requests by a scan of one wavefront, and its threads walk over
-// those requests' tokens as one sequence.  blockIdx.y divides that sequence: one long prompt is written by many workgroups.
+// (two integers of each, from the caches), then places its own by scans of one wavefront, kChunk at a time, and its threads walk over
+// their tokens as one sequence.  blockIdx.y divides that sequence: one long prompt is written by many workgroups.  There are no more than
+// kMostGroups workgroups along the requests, so that what they read in front of their own stays in proportion to the requests: beyond
+// 16 * kMostGroups of them each takes several chunks.
 // No workgroup reads what another writes: pages given out in this call are looked up in the free list, not in the table.
 #include "pq_kv4.h"
 
@@ -18,7 +20,8 @@ namespace kv4 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 16;       // requests of a workgroup
+constexpr int kChunk = 16;       // requests that a workgroup places at a time
+constexpr int kMostGroups = 2048;
 
 struct Request {
     int64_t kv, q;
@@ -42,17 +45,17 @@ __device__ __forceinline__ int32_t saturate(int64_t v) { return (int32_t)min(v, 
 __global__ __launch_bounds__(kThreads) void k_kv4_slots(const int32_t* __restrict__ kv_len, const int32_t* __restrict__ q_len, int B,
                                                         int32_t* table, int W, const int32_t* __restrict__ free_pages, int n_free,
                                                         const int32_t* taken, int log2_page, int T, int position_offset, int32_t* cu_q,
-                                                        int32_t* kv_len_out, int32_t* positions, int64_t* slots, int32_t* taken_out)
+                                                        int32_t* kv_len_out, int32_t* positions, int64_t* slots, int32_t* taken_out, int chunks)
 {
     __shared__ int64_t wave_q[kThreads / 64], wave_need[kThreads / 64];
     __shared__ int64_t start_s[kChunk + 1], first_s[kChunk];       // of the workgroup's requests: cu_q and place in the free list
     __shared__ int64_t kv_s[kChunk];
     __shared__ int32_t before_s[kChunk], need_s[kChunk];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int b0 = blockIdx.x * kChunk, own = min(kChunk, B - b0);
+    const int own_first = blockIdx.x * chunks * kChunk, own_end = min(own_first + chunks * kChunk, B);
 
     int64_t q_sum = 0, need_sum = 0;
-    for (int b = tid; b < b0; b += kThreads) {
+    for (int b = tid; b < own_first; b += kThreads) {
         const Request r = request(kv_len, q_len, b, W, log2_page);
         q_sum += r.q;
         need_sum += r.need;
@@ -67,75 +70,85 @@ __global__ __launch_bounds__(kThreads) void k_kv4_slots(const int32_t* __restric
         wave_need[tid >> 6] = need_sum;
     }
     __syncthreads();
+    int64_t start = 0, first = 0;                                  // of the next chunk, in the first wavefront
     if (tid < 64) {
-        int64_t start = 0, first = taken ? *taken : 0;
+        first = taken ? *taken : 0;
 #pragma unroll
         for (int w = 0; w < kThreads / 64; ++w) {
             start += wave_q[w];
             first += wave_need[w];
         }
-        Request r = {0, 0, 0, 0};
-        if (lane < own) r = request(kv_len, q_len, b0 + lane, W, log2_page);
-        int64_t q_incl = r.q, need_incl = r.need;
+    }
+    const int slice = blockIdx.y * kThreads + tid, threads = gridDim.y * kThreads;
+    for (int b0 = own_first;; b0 += kChunk) {
+        const int own = min(kChunk, own_end - b0);                 // (none if there are no requests)
+        if (tid < 64) {
+            Request r = {0, 0, 0, 0};
+            if (lane < own) r = request(kv_len, q_len, b0 + lane, W, log2_page);
+            int64_t q_incl = r.q, need_incl = r.need;
 #pragma unroll
-        for (int d = 1; d < kChunk; d <<= 1) {
-            const int64_t a = __shfl_up(q_incl, d, 64), c = __shfl_up(need_incl, d, 64);
-            if (lane >= d) {
-                q_incl += a;
-                need_incl += c;
+            for (int d = 1; d < kChunk; d <<= 1) {
+                const int64_t a = __shfl_up(q_incl, d, 64), c = __shfl_up(need_incl, d, 64);
+                if (lane >= d) {
+                    q_incl += a;
+                    need_incl += c;
+                }
+            }
+            if (lane < kChunk) {
+                start_s[lane] = start + q_incl - r.q;
+                first_s[lane] = first + need_incl - r.need;
+                kv_s[lane] = r.kv;
+                before_s[lane] = r.before;
+                need_s[lane] = r.need;
+                if (lane == kChunk - 1) start_s[kChunk] = start + q_incl;
+            }
+            if (lane < own && blockIdx.y == 0) {
+                cu_q[b0 + lane] = saturate(start + q_incl - r.q);
+                kv_len_out[b0 + lane] = saturate(r.kv + r.q);
+            }
+            if (lane == kChunk - 1 && blockIdx.y == 0 && b0 + own == B) {
+                cu_q[B] = saturate(start + q_incl);
+                *taken_out = saturate(first + need_incl);
+            }
+            start += __shfl(q_incl, kChunk - 1, 64);
+            first += __shfl(need_incl, kChunk - 1, 64);
+        }
+        __syncthreads();
+
+        // new entries of the table: one wavefront to a request
+        for (int j = slice >> 6; j < own; j += threads >> 6) {
+            const int64_t from = first_s[j];
+            for (int i = lane; i < need_s[j]; i += 64) {
+                const int64_t at = from + i;
+                table[(int64_t)(b0 + j) * W + before_s[j] + i] = at >= 0 && at < n_free ? free_pages[at] : -1;
             }
         }
-        if (lane < kChunk) {
-            start_s[lane] = start + q_incl - r.q;
-            first_s[lane] = first + need_incl - r.need;
-            kv_s[lane] = r.kv;
-            before_s[lane] = r.before;
-            need_s[lane] = r.need;
-            if (lane == kChunk - 1) start_s[kChunk] = start + q_incl;
-        }
-        if (lane < own && blockIdx.y == 0) {
-            cu_q[b0 + lane] = saturate(start + q_incl - r.q);
-            kv_len_out[b0 + lane] = saturate(r.kv + r.q);
-        }
-        if (lane == kChunk - 1 && blockIdx.y == 0 && b0 + own == B) {
-            cu_q[B] = saturate(start + q_incl);
-            *taken_out = saturate(first + need_incl);
-        }
-    }
-    __syncthreads();
-
-    const int slice = blockIdx.y * kThreads + tid, threads = gridDim.y * kThreads;
-    // new entries of the table: one wavefront to a request
-    for (int j = slice >> 6; j < own; j += threads >> 6) {
-        const int64_t first = first_s[j];
-        for (int i = lane; i < need_s[j]; i += 64) {
-            const int64_t at = first + i;
-            table[(int64_t)(b0 + j) * W + before_s[j] + i] = at >= 0 && at < n_free ? free_pages[at] : -1;
-        }
-    }
-    // tokens
-    const int64_t begin = start_s[0], end = min(start_s[kChunk], (int64_t)T);
-    for (int64_t t = begin + slice; t < end; t += threads) {
-        int j = 0;
+        // tokens
+        const int64_t begin = start_s[0], end = min(start_s[kChunk], (int64_t)T);
+        for (int64_t t = begin + slice; t < end; t += threads) {
+            int j = 0;
 #pragma unroll
-        for (int d = kChunk / 2; d >= 1; d >>= 1) j += start_s[j + d] <= t ? d : 0;
-        const int64_t at = kv_s[j] + t - start_s[j], col = at >> log2_page;
-        int64_t page = -1;
-        if (col < before_s[j]) {
-            page = table[(int64_t)(b0 + j) * W + col];
-        } else if (col < before_s[j] + need_s[j]) {
-            const int64_t i = first_s[j] + col - before_s[j];
-            if (i >= 0 && i < n_free) page = free_pages[i];
+            for (int d = kChunk / 2; d >= 1; d >>= 1) j += start_s[j + d] <= t ? d : 0;
+            const int64_t at = kv_s[j] + t - start_s[j], col = at >> log2_page;
+            int64_t page = -1;
+            if (col < before_s[j]) {
+                page = table[(int64_t)(b0 + j) * W + col];
+            } else if (col < before_s[j] + need_s[j]) {
+                const int64_t i = first_s[j] + col - before_s[j];
+                if (i >= 0 && i < n_free) page = free_pages[i];
+            }
+            positions[t] = saturate(position_offset + at);
+            slots[t] = page >= 0 ? (page << log2_page) + (at & ((1ll << log2_page) - 1)) : -1;
         }
-        positions[t] = saturate(position_offset + at);
-        slots[t] = page >= 0 ? (page << log2_page) + (at & ((1ll << log2_page) - 1)) : -1;
-    }
-    // rows behind the last request
-    if (b0 + own == B) {
-        for (int64_t t = start_s[kChunk] + slice; t < T; t += threads) {
-            positions[t] = 0;
-            slots[t] = -1;
+        // rows behind the last request
+        if (b0 + own == B) {
+            for (int64_t t = start_s[kChunk] + slice; t < T; t += threads) {
+                positions[t] = 0;
+                slots[t] = -1;
+            }
         }
+        if (b0 + kChunk >= own_end) break;
+        __syncthreads();                                           // (read before the next chunk takes their place)
     }
 }
 
@@ -145,16 +158,16 @@ int launch_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t
                  const int32_t* free_pages, int32_t n_free, const int32_t* taken, int32_t log2_page, int32_t T, int32_t position_offset,
                  int32_t* cu_q, int32_t* kv_len_out, int32_t* positions, int64_t* slots, int32_t* taken_out, hipStream_t st)
 {
-    const int chunks = B > 0 ? (B + kChunk - 1) / kChunk : 1;
-    // about four tokens to a thread, and no more than eight workgroups to a CU over all chunks
-    const int64_t per_chunk = ((int64_t)T + chunks - 1) / chunks;
-    int64_t slices = (per_chunk + 4 * kThreads - 1) / (4 * kThreads), most = 2048 / chunks;
+    const int all = B > 0 ? (B + kChunk - 1) / kChunk : 1, chunks = (all + kMostGroups - 1) / kMostGroups, groups = (all + chunks - 1) / chunks;
+    // about four tokens to a thread, and no more than eight workgroups to a CU in all
+    const int64_t per_group = ((int64_t)T + groups - 1) / groups;
+    int64_t slices = (per_group + 4 * kThreads - 1) / (4 * kThreads), most = kMostGroups / groups;
     if (most < 1) most = 1;
     if (slices < 1) slices = 1;
     if (slices > most) slices = most;
-    k_kv4_slots<<<dim3((unsigned)chunks, (unsigned)slices), kThreads, 0, st>>>(kv_len, q_len, B, block_table, table_pages, free_pages, n_free,
+    k_kv4_slots<<<dim3((unsigned)groups, (unsigned)slices), kThreads, 0, st>>>(kv_len, q_len, B, block_table, table_pages, free_pages, n_free,
                                                                                taken, log2_page, T, position_offset, cu_q, kv_len_out, positions,
-                                                                               slots, taken_out);
+                                                                               slots, taken_out, chunks);
     return hip_status(hipGetLastError());
 }
 

@@ -6,7 +6,7 @@ import torch
 
 import kv4_reference as R
 from pq_testlib import dev, host
-from test_gpu_kv4 import append_case, attention_case, call, i32, pq, put, rope_table            # noqa: F401 (pq: a fixture)
+from test_gpu_kv4 import append_case, attention_case, call, check_slots, i32, lengths, pq, put, rope_table   # noqa: F401 (pq: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -138,3 +138,11 @@ def test_a_step_with_too_few_rows_or_pages(pq, group, T, W):
     want, bound, real = R.attention(whole, host(cu), host(kv_all), wide, host(kc), host(vc), host(ks), host(vs), D ** -0.5, group)
     got = host(out).astype(np.float64).reshape(want[:T].shape)
     assert np.all((np.abs(got - want[:T]) <= bound[:T])[real[:T]])
+
+
+# ------------------------------------------------------------------------------------------------ very many requests
+@pytest.mark.parametrize("B,q,short", [(32768, 3, 0), (32769, 3, 0), (40001, 5, 20000), (100003, 4, 0), (131072, 2, 100000)])
+def test_slots_of_more_requests_than_workgroups(pq, B, q, short):
+    """A workgroup places several chunks of requests one after another; a list that ends among them."""
+    kv, n = lengths(B, 60, q, B)
+    check_slots(pq, kv, n, 5, 16, 2 * B - short, int(n.sum()) + 77, taken=3, offset=2, seed=B)
