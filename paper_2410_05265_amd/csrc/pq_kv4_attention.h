@@ -33,6 +33,11 @@ typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kTileRows = 256;           // rows of a workgroup of the kernel for many queries
 
+// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and the others the row kernel.  Row | tile kernel, us,
+// 32 heads of 128 on 8: one request of 33000 tokens with 128 rows 56 | 107, 192 63 | 110, 256 77 | 79; 8 of up to 4000 46 | 63, 52 | 54,
+// 60 | 55; 64 of up to 2000 113 | 137, 146 | 140, 185 | 148; with a step to 32 channels 218 | 307, 284 | 322, 372 | 330.
+constexpr int kSmallRows = 192;
+
 constexpr float kNothing = -1e30f;       // reference before the first score
 constexpr float kMost = 14.0f, kBack = 6.0f;
 constexpr float kUnit = 0x1.0p20f;       // a code as operand is u * 2^-20

@@ -716,11 +716,6 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
 // requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
 int blocks_for(int32_t max_q, int32_t per_kv, int64_t units) { return (int64_t)max_q * per_kv > 16 && units > 48 * kGroups * kWaves ? 2 : 1; }
 
-// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and this one the others.  This | tile kernel, us,
-// 32 heads of 128 on 8: one request of 33000 tokens with 128 rows 56 | 107, 192 63 | 110, 256 77 | 79; 8 of up to 4000 46 | 63, 52 | 54,
-// 60 | 55; 64 of up to 2000 113 | 137, 146 | 140, 185 | 148; with a step to 32 channels 218 | 307, 284 | 322, 372 | 330.
-constexpr int kSmallRows = 192;
-
 bool takes_tiles(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv > kSmallRows; }
 // A single request is the tile kernel's whatever its rows are: the two launches that would find nothing to do take 4 us (1024 tokens of one
 // prompt, 32 heads on 8: 38 us with them, 34 without).

@@ -552,9 +552,17 @@ __global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_tiles(Atten
     }
 }
 
-int64_t tiles_at_most(int64_t T, int32_t B, int32_t per_kv) { return (T * per_kv + (int64_t)(kRows - 1) * B) / kRows; }
+// Tiles of rows, at most.  Of several requests only those of more than 192 rows come here, and R such rows are at most 2 R / 257 tiles
+// (two of 257): requests that decode beside a prompt do not count as a tile each.
+int64_t tiles_at_most(int64_t T, int32_t B, int32_t per_kv)
+{
+    const int64_t by_requests = (T * per_kv + (int64_t)(kRows - 1) * B) / kRows, by_rows = 2 * T * per_kv / (kRows + 1);
+    static_assert(2 * (kSmallRows + 1) >= kRows + 1, "one tile of the fewest rows");
+    return B == 1 || by_requests < by_rows ? by_requests : by_rows > 1 ? by_rows : 1;
+}
 
-// Parts of a history, of at least eight tiles of tokens each.  Several requests differ in length: about two workgroups to a CU even that
+// Parts of a history, of at least eight tiles of tokens each where the table is as long as the history (the host knows the table; parts of
+// shorter ones are shorter, or empty).  Several requests differ in length: about two workgroups to a CU even that
 // out (B 4, 300 queries each over up to 4000 tokens, 32 on 8 heads: one part 127 us, two 103, three 112).  The parts of one request are
 // alike: as many as fill whole rounds of one workgroup to a CU, which is what its registers allow, with eight tiles' time for what every
 // workgroup does once (500 queries over 33000 tokens, 64 on 8 heads: one part 910 us, two 534, four 541; 64 queries over 131072, 32 on 8

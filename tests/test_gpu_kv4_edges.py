@@ -146,3 +146,13 @@ def test_slots_of_more_requests_than_workgroups(pq, B, q, short):
     """A workgroup places several chunks of requests one after another; a list that ends among them."""
     kv, n = lengths(B, 60, q, B)
     check_slots(pq, kv, n, 5, 16, 2 * B - short, int(n.sum()) + 77, taken=3, offset=2, seed=B)
+
+
+# ------------------------------------------------------------------------------------------------ prompts beside decoding requests
+@pytest.mark.parametrize("D,group", [(64, 0), (128, 0), (128, 32)])
+@pytest.mark.parametrize("q_lens", [[1] * 7 + [60] + [1] * 24, [49, 1, 65, 2, 1, 129, 48, 0, 1], [1] * 40 + [50, 49, 51]])
+def test_prompts_beside_decoding_requests(pq, D, group, q_lens):
+    """Requests of 4 heads a key/value head: more than 48 queries take the kernel for many rows, in parts, the others the one for few."""
+    r = np.random.default_rng(len(q_lens))
+    kv = [m + int(r.integers(0, 900 if m > 2 else 200)) for m in q_lens]
+    check_cut(pq, attention_case(kv, q_lens, 4, 1, D, 3, group, 64, W=64, prefix=3), hints=(max(q_lens),))
