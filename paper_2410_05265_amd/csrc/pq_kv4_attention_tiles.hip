@@ -42,8 +42,50 @@ __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r
     return rows <= small_rows ? 0 : (int)((rows + kRows - 1) / kRows);
 }
 
-__device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index, int small_rows, int lane)
+// For many requests: `starts`, tiles before each request and in all.  A workgroup that walks over the requests itself reads all of them, and
+// there may be as many workgroups; with this list it reads some ten or twenty entries.  Without | with it, us, 4 heads of 128 on one, 60
+// queries each over 200 tokens: 256 requests 32 | 34, 512 61 | 60, 1024 124 | 107, 2048 361 | 221, 16384 9700 | 1520, 65536 136000 | 5900.
+constexpr int kManyRequests = 512;
+constexpr int kStartThreads = 1024;
+__global__ __launch_bounds__(kStartThreads) void k_kv4_attention_tile_starts(AttentionArgs a, int32_t* starts, int small_rows)
 {
+    __shared__ int64_t sums[kStartThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, each = (a.B + kStartThreads - 1) / kStartThreads;
+    const int first = min(tid * each, a.B), last = min(first + each, a.B);
+    int64_t own = 0;
+    for (int b = first; b < last; ++b) own += tiles_of(a, request(a, b), small_rows);
+    int64_t incl = own;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t v = __shfl_up(incl, d, 64);
+        if (lane >= d) incl += v;
+    }
+    if (lane == 63) sums[tid >> 6] = incl;
+    __syncthreads();
+    int64_t at = incl - own;
+    for (int w = 0; w < tid >> 6; ++w) at += sums[w];
+    auto saturate = [](int64_t v) PQ_INLINE { return (int32_t)min(v, (int64_t)INT32_MAX); };   // (of rows that lie in several requests)
+    for (int b = first; b < last; ++b) {
+        starts[b] = saturate(at);
+        at += tiles_of(a, request(a, b), small_rows);
+    }
+    if (tid == kStartThreads - 1) starts[a.B] = saturate(at);
+}
+
+__device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index, int small_rows, const int32_t* __restrict__ starts, int lane)
+{
+    if (starts != nullptr) {
+        if (index >= starts[a.B]) return {-1, 0, {0, 0, 0, 0}};
+        int lo = 0, hi = a.B - 1;                  // the first request that ends behind the index
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (starts[mid + 1] > index) hi = mid;
+            else lo = mid + 1;
+        }
+        const Request r = request(a, lo);
+        const int n = tiles_of(a, r, small_rows), tile = n - 1 - (int)(index - starts[lo]);
+        return {tile >= 0 && tile < n ? lo : -1, tile, r};
+    }
     const int each = (a.B + 63) / 64, first = min(lane * each, a.B), last = min(first + each, a.B);
     Request r = {0, 0, 0, 0};                       // the last of this lane's; up to 64 requests are read once
     int64_t own = 0;
@@ -113,7 +155,7 @@ struct Lds {
 // static steps, one | two: 4 prompts of up to 4096 tokens 296 | 252 us, 300 queries each over up to 4000 83 | 75, 500 over 33000 240 | 243;
 // with dynamic steps what does not fit is spilled: 409 | 764).
 template <int D, int G, bool DYNAMIC>
-__global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs a, float* partial, int splits, int small_rows)
+__global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs a, float* partial, const int32_t* __restrict__ starts, int splits, int small_rows)
 {
     constexpr int NG = D / G, KS = D / 16, KSG = G / 16, DB = D / 32, DBG = G / 32;
     extern __shared__ __align__(256) uint8_t raw_lds[];
@@ -124,7 +166,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     const int log2_page = a.cache.log2_page, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv;
     const int head = blockIdx.x % Hkv, split = (blockIdx.x / Hkv) % splits;
     const int64_t index = blockIdx.x / Hkv / splits;
-    const Where at = find_tile(a, index, small_rows, lane);
+    const Where at = find_tile(a, index, small_rows, starts, lane);
     if (at.b < 0) return;
     const Request r = at.r;
     const int rows = r.q_len * per_kv, row0 = at.tile * kRows;
@@ -516,13 +558,14 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
 
 // Adds the parts of a tile's rows: a workgroup takes 64 rows, a wavefront a quarter of the channels.
 template <int D, int G>
-__global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_tiles(AttentionArgs a, const float* __restrict__ partial, int splits, int small_rows)
+__global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_tiles(AttentionArgs a, const float* __restrict__ partial, const int32_t* __restrict__ starts, int splits,
+                                                                            int small_rows)
 {
     __shared__ __align__(16) __half lines[64][D + 8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, Hkv = a.cache.n_kv_heads;
     const int head = blockIdx.x % Hkv;
     const int64_t index = blockIdx.x / Hkv;
-    const Where at = find_tile(a, index, small_rows, lane);
+    const Where at = find_tile(a, index, small_rows, starts, lane);
     if (at.b < 0) return;
     const int rows = at.r.q_len * a.heads_per_kv, row0 = at.tile * kRows + blockIdx.y * 64;
     if (row0 >= rows) return;
@@ -585,16 +628,22 @@ int splits_for(int64_t tiles, int32_t B, int32_t n_kv_heads, int64_t capacity)
 }
 
 template <int D, int G, bool DYNAMIC>
-int launch(const AttentionArgs& a, int64_t tiles, int splits, int small_rows, float* partial, hipStream_t st)
+int launch(const AttentionArgs& a, int64_t tiles, int splits, int small_rows, float* partial, const int32_t* starts, hipStream_t st)
 {
     static std::atomic<uint64_t> allowed{0};
     const size_t out = (size_t)kWaves * kCols * (D + 8) * 2, lds = sizeof(Lds<D, G, DYNAMIC>) > out ? sizeof(Lds<D, G, DYNAMIC>) : out;
     const auto kernel = k_kv4_attention_tiles<D, G, DYNAMIC>;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, allowed); rc != PQ_OK) return rc;
     const int Hkv = a.cache.n_kv_heads;
-    kernel<<<(unsigned)(tiles * Hkv * splits), kThreads, lds, st>>>(a, partial, splits, small_rows);
-    if (splits > 1) k_kv4_attention_join_tiles<D, G><<<dim3((unsigned)(tiles * Hkv), kRows / 64), kJoinThreads, 0, st>>>(a, partial, splits, small_rows);
+    kernel<<<(unsigned)(tiles * Hkv * splits), kThreads, lds, st>>>(a, partial, starts, splits, small_rows);
+    if (splits > 1) k_kv4_attention_join_tiles<D, G><<<dim3((unsigned)(tiles * Hkv), kRows / 64), kJoinThreads, 0, st>>>(a, partial, starts, splits, small_rows);
     return hip_status(hipGetLastError());
+}
+
+// Scratch memory: partial sums, then the list of starts.
+size_t tiles_partial_bytes(int64_t tiles, int splits, int32_t n_kv_heads, int32_t head_dim)
+{
+    return splits > 1 ? (size_t)(tiles * n_kv_heads * splits) * kRows * (head_dim + 2) * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -603,22 +652,27 @@ size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv
 {
     const int64_t tiles = tiles_at_most(T, B, n_heads / n_kv_heads);
     const int splits = splits_for(tiles, B, n_kv_heads, capacity);
-    return splits > 1 ? (size_t)(tiles * n_kv_heads * splits) * kRows * (head_dim + 2) * sizeof(float) : 0;
+    return tiles_partial_bytes(tiles, splits, n_kv_heads, head_dim) + (B > kManyRequests ? ((size_t)(B + 1) * sizeof(int32_t) + 255) & ~(size_t)255 : 0);
 }
 
 int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st)
 {
     const int64_t tiles = tiles_at_most(a.T, a.B, a.heads_per_kv);
     const int splits = splits_for(tiles, a.B, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
-    if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false>(a, tiles, splits, small_rows, partial, st);
-        if (group == 32) return launch<64, 32, true>(a, tiles, splits, small_rows, partial, st);
-        return launch<64, 64, true>(a, tiles, splits, small_rows, partial, st);
+    int32_t* starts = nullptr;
+    if (a.B > kManyRequests) {
+        starts = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(partial) + tiles_partial_bytes(tiles, splits, a.cache.n_kv_heads, head_dim));
+        k_kv4_attention_tile_starts<<<1, kStartThreads, 0, st>>>(a, starts, small_rows);
     }
-    if (group == 0) return launch<128, 128, false>(a, tiles, splits, small_rows, partial, st);
-    if (group == 32) return launch<128, 32, true>(a, tiles, splits, small_rows, partial, st);
-    if (group == 64) return launch<128, 64, true>(a, tiles, splits, small_rows, partial, st);
-    return launch<128, 128, true>(a, tiles, splits, small_rows, partial, st);
+    if (head_dim == 64) {
+        if (group == 0) return launch<64, 64, false>(a, tiles, splits, small_rows, partial, starts, st);
+        if (group == 32) return launch<64, 32, true>(a, tiles, splits, small_rows, partial, starts, st);
+        return launch<64, 64, true>(a, tiles, splits, small_rows, partial, starts, st);
+    }
+    if (group == 0) return launch<128, 128, false>(a, tiles, splits, small_rows, partial, starts, st);
+    if (group == 32) return launch<128, 32, true>(a, tiles, splits, small_rows, partial, starts, st);
+    if (group == 64) return launch<128, 64, true>(a, tiles, splits, small_rows, partial, starts, st);
+    return launch<128, 128, true>(a, tiles, splits, small_rows, partial, starts, st);
 }
 
 }  // namespace kv4

@@ -156,3 +156,36 @@ def test_prompts_beside_decoding_requests(pq, D, group, q_lens):
     r = np.random.default_rng(len(q_lens))
     kv = [m + int(r.integers(0, 900 if m > 2 else 200)) for m in q_lens]
     check_cut(pq, attention_case(kv, q_lens, 4, 1, D, 3, group, 64, W=64, prefix=3), hints=(max(q_lens),))
+
+
+@pytest.mark.parametrize("D,group", [(64, 0), (128, 64)])
+def test_prompts_among_very_many_requests(pq, D, group):
+    """More than 512 requests, whose tiles of rows the kernel for many rows looks up in a list: a few prompts, in parts, among others."""
+    r = np.random.default_rng(5)
+    q_lens = r.integers(0, 3, 600)
+    q_lens[[0, 17, 18, 333, 599]] = [70, 49, 130, 48, 65]
+    kv = q_lens + r.integers(0, 30, 600)
+    kv[[17, 599]] += 700
+    check_cut(pq, attention_case(kv, q_lens, 4, 1, D, 4, group, 16, W=128, prefix=1), hints=(130,))
+
+
+@pytest.mark.parametrize("group", [0, 64])
+def test_very_many_prompts(pq, group):
+    """1300 requests of more rows than the kernel for few takes, some of none: bit for bit what they are 100 at a time."""
+    B, D, ps, pages = 1300, 64, 16, 900
+    r = np.random.default_rng(6)
+    q_lens = np.where(r.random(B) < 0.1, 0, r.integers(49, 140, B))
+    kv = q_lens + r.integers(0, 60, B)
+    table = r.integers(0, pages, (B, 16)).astype(np.int32)
+    kc, vc = (dev(r.integers(0, 256, (pages, 2, ps, D // 2)).astype(np.uint8)) for _ in range(2))
+    ks, vs = (dev(r.uniform(0.2, 0.6, (pages, 2, ps, D // group) if group else 2).astype(np.float32)) for _ in range(2))
+    cu = np.concatenate([[0], np.cumsum(q_lens)])
+    q = dev((1.5 * r.standard_normal((cu[-1], 8 * D))).astype(np.float16))
+
+    def part(lo, hi):
+        return pq.pq_kv4_attention(q[cu[lo]:cu[hi]], i32(cu[lo:hi + 1] - cu[lo]), i32(kv[lo:hi]), dev(table[lo:hi]), kc, vc, ks, vs, D ** -0.5, 139,
+                                   group=group)[0]
+
+    whole = part(0, B)
+    assert bool(whole.any(dim=1).all())
+    assert torch.equal(whole, torch.cat([part(lo, lo + 100) for lo in range(0, B, 100)]))

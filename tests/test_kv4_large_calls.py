@@ -36,3 +36,12 @@ def test_every_tile_of_rows_has_a_workgroup():
     for per_kv, lens in ((4, [49] * 40), (4, [65] * 30 + [1] * 30), (1, [193] * 9), (1, [257] * 12 + [3]), (1, [192, 192]), (8, [33, 32]), (1, [513, 1])):
         tiles, _ = tiles_and_parts(T=sum(lens), B=len(lens), max_q=max(max(lens), 200), Hq=8 * per_kv)
         assert tiles >= sum(-(-n * per_kv // 256) for n in lens if n * per_kv > 192)
+
+
+def test_many_requests_get_a_list_of_their_tiles():
+    """Beyond 512 requests no workgroup of the kernel for many rows walks over all of them."""
+    for B, listed in ((2, 0), (512, 0), (513, 1), ((1 << 21) // 8 - 1, 1)):
+        (rc, need, events), = launches([dict(fn="attention", T=60 * B, B=B, Hq=32, Hkv=8, D=128, group=0, ps=64, W=4, max_q=60)])
+        names = [e[1] for e in events if e[0] == "launch"]
+        assert rc == 0 and names.count("k_kv4_attention_tile_starts") == listed
+        assert not listed or names.index("k_kv4_attention_tile_starts") == 0 and need >= 4 * (B + 1)
