@@ -277,12 +277,13 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         }
 
         float m[CB], l[CB];                        // l: of this lane's tokens
+        float l_prefix[CB];                        // static steps: of the prefix tokens, whose values have no offset
         v4f o[CB][NG * CH];
         float ref[CB][NG], lw[CB][NG];             // dynamic steps: weights p * step are rounded relative to ref
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             m[c] = kNothing;
-            l[c] = 0.0f;
+            l[c] = l_prefix[c] = 0.0f;
 #pragma unroll
             for (int i = 0; i < NG * CH; ++i) o[c][i] = (v4f){0, 0, 0, 0};
 #pragma unroll
@@ -315,6 +316,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                         for (int i = 0; i < CH; ++i) o[c][g * CH + i] *= f;
                     }
                 } else {
+                    l_prefix[c] *= alpha;
 #pragma unroll
                     for (int i = 0; i < NG * CH; ++i) o[c][i] *= alpha;
                 }
@@ -379,18 +381,19 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read before the next values, or codes, take their place)
             }
-            // as if they were codes: sum p v = step (unit acc - 8 sum p) has to hold
+            // in units of a code; their sum of p apart, so that no offset is added here to be taken off again: its rounding would be 2^-21 of
+            // a step, and where these tokens have the weight their values may be far smaller
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
-                float l_all = l[c] + __shfl_xor(l[c], 16, 64);
-                l_all += __shfl_xor(l_all, 32, 64);
-                const float times = DYNAMIC ? 1.0f / (kUnit * kLeast) : 1.0f / (kUnit * v_step), plus = DYNAMIC ? 0.0f : 8.0f / kUnit * l_all;
+                const float times = DYNAMIC ? 1.0f / (kUnit * kLeast) : 1.0f / (kUnit * v_step);
 #pragma unroll
-                for (int i = 0; i < NG * CH; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) o[c][i][k] = fmaf(o[c][i][k], times, plus);
+                for (int i = 0; i < NG * CH; ++i) o[c][i] *= times;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) ref[c][g] = kLeast;
+                if constexpr (!DYNAMIC) {
+                    l_prefix[c] = l[c];
+                    l[c] = 0.0f;
+                }
             }
             for (int i = early; i < min(count, kDepth); ++i) fetch(i);
         }
@@ -554,9 +557,14 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         for (int c = 0; c < CB; ++c) {
             l[c] += __shfl_xor(l[c], 16, 64);
             l[c] += __shfl_xor(l[c], 32, 64);
+            float l_all = l[c];
+            if constexpr (!DYNAMIC) {
+                l_prefix[c] += __shfl_xor(l_prefix[c], 16, 64);
+                l_all += l_prefix[c] + __shfl_xor(l_prefix[c], 32, 64);
+            }
             const int row = tile * ROWS + 16 * c + col;
             const bool live = row < rows;
-            const float f = take == per ? (l[c] > 0.0f ? v_step / l[c] : 0.0f) : v_step;
+            const float f = take == per ? (l_all > 0.0f ? v_step / l_all : 0.0f) : v_step;
             float* const part = partial + (((int64_t)worker * 2 + (u0 == range ? 0 : 1)) * ROWS + 16 * c + col) * (D + 4);
             __half* const dst = a.out + ((int64_t)(r.start + min(row, rows - 1) / per_kv) * a.n_heads + head * per_kv + min(row, rows - 1) % per_kv) * D;
 #pragma unroll
@@ -592,7 +600,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             }
             if (live && take != per && quarter == 0) {
                 part[0] = m[c];
-                part[1] = l[c];
+                part[1] = l_all;
             }
         }
         u0 += take;

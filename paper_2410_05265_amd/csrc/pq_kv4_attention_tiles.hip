@@ -296,6 +296,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     }
 
     float m = kNothing, l = 0.0f;
+    float l_prefix = 0.0f;                   // static steps: of the prefix tokens, whose values have no offset
     float ref[NG];                           // dynamic steps: weights p * step are rounded relative to ref
     v16f o[DB];
 #pragma unroll
@@ -325,6 +326,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
                     for (int i = 0; i < DBG; ++i) o[g * DBG + i] *= f;
                 }
             } else {
+                l_prefix *= alpha;
 #pragma unroll
                 for (int i = 0; i < DB; ++i) o[i] *= alpha;
             }
@@ -439,15 +441,18 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             multiply(0, 0, DB, p);
         }
         __syncthreads();
-        // as if they were codes: sum p v = step (unit acc - 8 sum p) has to hold
-        const float l_all = l + __shfl_xor(l, 32, 64);
-        const float times = DYNAMIC ? 1.0f / (kUnit * kLeast) : 1.0f / (kUnit * v_step), plus = DYNAMIC ? 0.0f : 8.0f / kUnit * l_all;
+        // in units of a code, their sum of p apart: no offset is added here to be taken off again (as in the kernel for few queries)
+        const float times = DYNAMIC ? 1.0f / (kUnit * kLeast) : 1.0f / (kUnit * v_step);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = fmaf(o[d][i], times, plus);
+            for (int i = 0; i < 16; ++i) o[d][i] *= times;
 #pragma unroll
         for (int g = 0; g < NG; ++g) ref[g] = kLeast;
+        if constexpr (!DYNAMIC) {
+            l_prefix = l;
+            l = 0.0f;
+        }
     }
 
     if (begin < end) {
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     }
 
     // ---- results
-    const float l_all = l + __shfl_xor(l, 32, 64);
+    const float l_codes = l + __shfl_xor(l, 32, 64), l_all = DYNAMIC ? l_codes : l_codes + (l_prefix + __shfl_xor(l_prefix, 32, 64));
     float times[NG], minus = 0.0f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -499,7 +504,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             times[g] = kUnit * ref[g];
         } else {
             times[g] = kUnit * v_step;
-            minus = 8.0f * v_step * l_all;
+            minus = 8.0f * v_step * l_codes;
         }
     }
     if (splits > 1) {

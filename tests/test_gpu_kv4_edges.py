@@ -140,6 +140,38 @@ def test_a_step_with_too_few_rows_or_pages(pq, group, T, W):
     assert np.all((np.abs(got - want[:T]) <= bound[:T])[real[:T]])
 
 
+# ------------------------------------------------------------------------------------------------ prefix tokens
+@pytest.mark.parametrize("D,group", [(64, 0), (128, 0), (64, 32), (128, 128)])
+@pytest.mark.parametrize("q_len", [1, 20, 60])
+@pytest.mark.parametrize("B", [1, 2])
+def test_prefix_values_far_smaller_than_the_steps(pq, D, group, q_len, B):
+    """The prefix tokens have nearly all the weight, as attention sinks do, and values below 2 * 10^-4 of a step: the result's error goes by
+    its own size, not by the steps'."""
+    P = 5
+    c = attention_case([3000, 700][:B], [q_len] * B, 4, 1, D, q_len, group, 64, prefix=P)
+    r = np.random.default_rng(1)
+    if group:
+        live = np.isfinite(c["vs"])
+        c["vs"][live] = 256.0
+        c["ks"][live] = 1e-3
+    else:
+        c["vs"][:], c["ks"][:] = 256.0, 1e-3
+    # Scores: queries and prefix keys have 1 in channel 0, scaled to 20 there; cached keys stay below 8e-3 * sum|q| * scale < 1.
+    scale = float(np.float32(c["scale"]))
+    c["q"] = (0.01 * r.standard_normal(c["q"].shape)).astype(np.float16)
+    c["q"].reshape(len(c["q"]), 4, D)[:, :, 0] = 16.0
+    c["pk"][:] = (0.01 * r.standard_normal(c["pk"].shape)).astype(np.float16)
+    c["pk"][:, :, 0] = np.float16(2.5 / scale)                     # 40: the cached tokens' weight is e^-40 * 3000 at most
+    c["pv"] = r.uniform(0.01, 0.05, c["pv"].shape).astype(np.float16)
+    want, _, real = R.attention(c["q"], c["cu"], c["kv"], c["table"], c["kc"], c["vc"], c["ks"], c["vs"], c["scale"], group, c["pk"], c["pv"])
+    got = host(call(pq, put(c), q_len)).astype(np.float64).reshape(want.shape)
+    err = np.abs(got - want)[real]
+    # Half a step of fp16 for each probability (static steps: they stand below the fraction too, so what counts is how far the values, 0.01 to
+    # 0.05, lie apart), and for the result, which is below 2^-4; scores of 40 to 2^-20, the cached tokens e^-39 * 3000 * 8 * 256 < 2^-30.
+    bound = (0.05 if group else 0.04) * 2.0 ** -11 * 1.01 + 2.0 ** -16 + 2 * 0.05 * 2.0 ** -20 + 2.0 ** -30
+    assert err.max() <= bound
+
+
 # ------------------------------------------------------------------------------------------------ very many requests
 @pytest.mark.parametrize("B,q,short", [(32768, 3, 0), (32769, 3, 0), (40001, 5, 20000), (100003, 4, 0), (131072, 2, 100000)])
 def test_slots_of_more_requests_than_workgroups(pq, B, q, short):
