@@ -497,14 +497,15 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             for (int g = 0; g < NG; ++g) {
                 if constexpr (DYNAMIC) {
                     float step[8];
-                    const int left = r.n - (t0 + 4 * quarter);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int e = (j & 3) * NG + g;
-                        step[j] = vs[j >> 2][e / 4][e % 4];
+                    for (int j = 0; j < 8; ++j) step[j] = vs[j >> 2][((j & 3) * NG + g) / 4][((j & 3) * NG + g) % 4];
+                    if (masked) {
                         // what lies behind the last token may be anything, and what only later queries see may be infinite: neither must
                         // meet a probability of zero as it is
-                        if (masked) step[j] = 16 * (j >> 2) + (j & 3) >= left || (j < 4 ? bad0 : bad1) ? 0.0f : finite_step(step[j]);
+                        const int left = r.n - (t0 + 4 * quarter);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) step[j] = 16 * (j >> 2) + (j & 3) >= left || (j < 4 ? bad0 : bad1) ? 0.0f : finite_step(step[j]);
+                        asm volatile("");          // (a branch: computed for every tile it costs one of 32 channels to a step 5 %)
                     }
 #pragma unroll
                     for (int c = 0; c < CB; ++c) {

@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     const Request r = at.r;
     const int rows = r.q_len * per_kv, row0 = at.tile * kRows;
     const int last_token = min((row0 + kRows - 1) / per_kv, r.q_len - 1);
-    const int visible = sees(a, r, last_token);
+    const int visible = __builtin_amdgcn_readfirstlane(sees(a, r, last_token));        // (a division leaves it in a vector register)
     const int all_tiles = (visible + kTile - 1) / kTile;
     const int begin = (int)((int64_t)all_tiles * split / splits), end = (int)((int64_t)all_tiles * (split + 1) / splits);
 
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
         const int row = min(row0 + wave * kCols + col, rows - 1);
         const int token = row / per_kv, q_head = head * per_kv + row % per_kv;
         limit = sees(a, r, token);
-        wave_sees = sees(a, r, min(row0 + wave * kCols, rows - 1) / per_kv);
+        wave_sees = __builtin_amdgcn_readfirstlane(sees(a, r, min(row0 + wave * kCols, rows - 1) / per_kv));
         const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h*>(src + 16 * s + 8 * half);
