@@ -1,6 +1,7 @@
 // C entry points of the paged 4-bit KV cache: argument checking only; every kernel goes to the caller's stream.
 #include "pq_kv4.h"
 
+#include <float.h>
 #include <math.h>
 
 namespace {
@@ -90,6 +91,8 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
         !aligned(positions, 4) || !aligned(slots, 8))
         return PQ_ERR_ALIGN;
     if (overlap(qkv_f16, (size_t)((T - 1) * row_stride + heads * D) * 2, q_out_f16, (size_t)(T * n_heads * D) * 2)) return PQ_ERR_UNSUPPORTED;
+    // (the reciprocal root takes subnormal numbers for zero; beside the least square of an fp16 number, 2^-48, no smaller eps shows)
+    if (eps > 0.0f && eps < FLT_MIN) eps = FLT_MIN;
     const pq::kv4::AppendArgs a = {static_cast<const __half*>(qkv_f16), row_stride, T, n_heads, positions, slots,
                                    static_cast<const __half*>(q_weight_f16), static_cast<const __half*>(k_weight_f16), eps, cos_sin,
                                    max_positions, rotary_dim, interleaved, clip, c, static_cast<__half*>(q_out_f16)};

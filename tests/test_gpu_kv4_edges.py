@@ -65,6 +65,22 @@ def test_append_infinities_stay_in_their_channel(pq, D, rd, interleaved, T):
         assert np.array_equal(got[number], want[number])
 
 
+def test_append_norm_of_zeros_with_the_smallest_eps(pq):
+    """x / sqrt(0 + eps) of zeros is zero for any eps above it, subnormal numbers among them."""
+    T, Hq, Hkv, D = 20, 4, 2, 128
+    c = append_case(T, Hq, Hkv, D, 3, 0)
+    c["qkv"][::2] = 0
+    w = np.ones(D, np.float16)
+    x = c["qkv"].reshape(T, Hq + 2 * Hkv, D)
+    for eps in (1e-38, 1e-40, 1.5e-45):
+        t = [dev(c[n]) for n in ("kc", "vc", "ks", "vs")]
+        q = host(pq.pq_kv4_append(dev(c["qkv"]), Hq, None, dev(c["slots"]), *t, q_weight=dev(w), k_weight=dev(w), eps=eps)).reshape(T, Hq, D)
+        z = R.turn(x[:, :Hq + Hkv], w, eps, None, None, False, True)
+        length = np.sqrt((z[:, :Hq] ** 2).sum(-1, keepdims=True))
+        assert np.all(np.abs(q.astype(np.float64) - z[:, :Hq]) <= 2.0 ** -20 * length + 2.0 ** -11 * np.abs(z[:, :Hq]) + 2.0 ** -25)
+        assert np.array_equal(R.unpack(host(t[0])[c["slots"] // 16, :, c["slots"] % 16]), R.codes_of(z[:, Hq:], c["ks"][None, :, None]))
+
+
 # ------------------------------------------------------------------------------------------------ steps that are cut off
 def check_cut(pq, c, T=None, W=None, hints=(1,), causal=True):
     """The first T rows of case c over the first W pages of its table, against the whole case whose table's other entries are none."""
