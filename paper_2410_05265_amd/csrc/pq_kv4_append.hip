@@ -11,7 +11,7 @@
 // order of the fp32 sums nor their contraction shows in the cache.
 //
 // Bound by HBM: 2 bytes of every channel in, 2 out for queries and half a byte for keys and values (8192 tokens x 48 heads of 128: 180 MB in
-// 46 us, 3.9 TB/s, where a copy of as many bytes takes 35); with norms and dynamic steps by vector instructions as well (2111 tokens x 80
+// 45 us, 4.0 TB/s, where a copy of as many bytes takes 35); with norms and dynamic steps by vector instructions as well (2111 tokens x 80
 // heads: 81 MB in 27 us); a step of 64 tokens by its launch and three dependent loads (4.5 us).  A lane holds eight channels
 // (16 bytes), D / 8 lanes a head, a wavefront the same head of 8 or 4 consecutive tokens: one kind of work to a wavefront, the step and
 // the norm's weights are read once, and in a page the tokens of a head lie one after another.  The four wavefronts of a workgroup take
@@ -158,6 +158,15 @@ __device__ __forceinline__ void halves_to_floats(const v4i raw, float (&v)[8])
     }
 }
 
+// A head's static step.  (Both addresses are read before one is chosen: a choice between two members of the arguments kept these in scratch
+// memory, 16 bytes of every lane, a fifth of what a long prompt's call wrote.)
+__device__ __forceinline__ float head_step(const AppendArgs& a, bool is_value, int kv_head)
+{
+    const float* const of_keys = a.cache.k_scale;
+    const float* const of_values = a.cache.v_scale;
+    return (is_value ? of_values : of_keys)[kv_head];
+}
+
 // Stores the codes of a wavefront's vectors, and the steps where they are dynamic.
 template <int LOG2_D, int LOG2_GROUP>
 __device__ __forceinline__ void store_codes(const AppendArgs& a, bool is_value, int64_t token, int c, uint32_t codes, float step)
@@ -190,7 +199,7 @@ __device__ __forceinline__ void append_exact(const AppendArgs& a, Lane& ln, Turn
     }
     float step;
     if constexpr (LOG2_GROUP == 0) {
-        step = (is_value ? a.cache.v_scale : a.cache.k_scale)[kv_head];
+        step = head_step(a, is_value, kv_head);
     } else {
         double most = 0.0;
 #pragma unroll
@@ -242,10 +251,9 @@ __device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, T
 
     const int kv_head = head - a.n_heads - (is_value ? Hkv : 0);
     const int64_t token = token0 + ((int64_t)kv_head << a.cache.log2_page);       // of this head in the cache
-    float* const scales = is_value ? a.cache.v_scale : a.cache.k_scale;
     float step;
     if constexpr (LOG2_GROUP == 0) {
-        step = scales[kv_head];
+        step = head_step(a, is_value, kv_head);
     } else {
         float most = 0.0f;
 #pragma unroll
@@ -276,10 +284,11 @@ __device__ __forceinline__ uint64_t append_head(const AppendArgs& a, Lane& ln, T
 
 // One head to a wavefront, or (MANY) eight, every fourth one: then what belongs to the token (its place, its angles) is read once for
 // them, the next head's values are on their way while one is turned, and the vectors for the fp64 path wait to the end, so that their
-// registers are not held in the loop.
+// registers are not held in the loop.  (Five wavefronts to a SIMD are asked for: left alone, static steps take 120 registers and four, 8192
+// tokens x 48 heads 48.3 us instead of 46.)
 constexpr int kMany = 8;
 template <int LOG2_D, int LOG2_GROUP, bool ROTATE, bool MANY>
-__global__ __launch_bounds__(kThreads) void k_kv4_append(AppendArgs a)
+__global__ __launch_bounds__(kThreads, MANY ? 5 : 1) void k_kv4_append(AppendArgs a)
 {
     constexpr int D = 1 << LOG2_D, kLanes = D / 8, kTokens = 64 / kLanes, kStride = kThreads / 64;
     const int lane = threadIdx.x & 63, c = lane & (kLanes - 1), heads = a.n_heads + 2 * a.cache.n_kv_heads;
@@ -371,10 +380,10 @@ int launch(const AppendArgs& a, hipStream_t st)
     const int64_t blocks = (a.T + kTokens - 1) / kTokens;
     const int heads = a.n_heads + 2 * a.cache.n_kv_heads;
     // Eight heads to a wavefront once one to each would be more than about two wavefronts to every place on the card (5 to 8 a SIMD, 1024
-    // SIMDs).  48 heads of 128, one | eight: 512 tokens (6144 wavefronts) 8.3 | 8.2 us, 1000 12.4 | 11.7, 2000 20.0 | 16.4, 8192 62 | 47,
-    // 16000 116 | 86; 80 heads with dynamic steps and norms: 512 tokens (10240) 11.8 | 13.1, 1000 18.8 | 17.7, 8000 107 | 86; 48 heads of
-    // 64: 512 tokens 6.3 | 7.7, 2000 (12000) 12.2 | 12.5, 8000 31.7 | 27.2.  With twelve a step of 64 tokens takes twice as long, with
-    // four 8192 tokens 50.
+    // SIMDs).  One | eight, us: 48 heads of 128, static steps, 200 tokens 5.0 | 7.8, 1000 (12000 wavefronts) 10.1 | 12.5, 2000 15.2 | 16.5, 8192
+    // 50 | 46, 16000 99 | 85; 80 heads with dynamic steps and norms: 512 tokens (10240) 10.8 | 13.1, 800 13.8 | 15.4, 1000 17.0 | 16.5, 8000
+    // 97 | 74; 48 heads of 64: 2000 tokens (12000) 9.5 | 11.9, 8000 26.2 | 26.2.  (The border is the lowest of any kind's: static steps without
+    // norms gain from about 40000 wavefronts on and lose up to a tenth between.)  With twelve a step of 64 tokens takes twice as long.
     const bool many = blocks * heads > 12288;
     const int each = 4 * (many ? kMany : 1);                             // heads of a workgroup
     const dim3 grid((unsigned)blocks, (unsigned)((heads + each - 1) / each));

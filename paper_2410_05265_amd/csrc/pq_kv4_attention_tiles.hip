@@ -192,30 +192,28 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     const int32_t* table = a.table + (int64_t)at.b * a.table_pages;
     const int block = wave & 3;
     const bool keys = wave < 4;
-    struct Codes { uint32_t w[4]; float s; int bad; };
+    struct Codes { v4u w; float s; int bad; };
     auto page_of = [&](int tile) PQ_INLINE { return table[min((tile * kTile + 16 * block) >> log2_page, a.table_pages - 1)]; };
     auto load = [&](int tile, int page, Codes& x) PQ_INLINE {
         const int t = tile * kTile + 16 * block;
         x.bad = (uint32_t)page >= (uint64_t)a.cache.n_pages || (t >> log2_page) >= a.table_pages;
         const int64_t from = x.bad ? 0 : page, first = ((from * Hkv + head) << log2_page) + (t & ((1 << log2_page) - 1));
+        // (one vector, set as a whole on both sides: an array's members went through scratch memory in every step)
         if (keys) {                                // D / 4 channels of a token to a lane
             const uint8_t* src = a.cache.k_codes + (first + (lane >> 2)) * (D / 2) + (lane & 3) * (D / 8);
             if constexpr (D == 128) {
-                const v4u w = *reinterpret_cast<const v4u*>(src);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x.w[i] = w[i];
+                x.w = *reinterpret_cast<const v4u*>(src);
             } else {
                 const v2u w = *reinterpret_cast<const v2u*>(src);
-                x.w[0] = w[0];
-                x.w[1] = w[1];
+                x.w = (v4u){w[0], w[1], 0, 0};
             }
         } else {                                   // D / 16 channels of four tokens
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            auto token = [&](int i) PQ_INLINE -> uint32_t {
                 const uint8_t* src = a.cache.v_codes + (first + 4 * (lane >> 4) + i) * (D / 2) + (lane & 15) * (D / 32);
-                if constexpr (D == 128) x.w[i] = *reinterpret_cast<const uint32_t*>(src);
-                else x.w[i] = *reinterpret_cast<const uint16_t*>(src);
-            }
+                if constexpr (D == 128) return *reinterpret_cast<const uint32_t*>(src);
+                else return *reinterpret_cast<const uint16_t*>(src);
+            };
+            x.w = (v4u){token(0), token(1), token(2), token(3)};
         }
         if constexpr (DYNAMIC) {                   // lane: token lane / 4, group lane % 4
             if ((lane & 3) < NG) x.s = (keys ? a.cache.k_scale : a.cache.v_scale)[(first + (lane >> 2)) * NG + (lane & 3)];
