@@ -532,7 +532,7 @@ int pq_calibrate_static_zp(const void* x_cal_f16, int64_t T, int64_t K, int32_t 
  * A cache of one layer: `n_pages` pages of `page_size` tokens (a power of two in [16, 1024]) for n_kv_heads heads of head_dim (64 or
  * 128) channels.
  *   k_codes, v_codes  uint8 [n_pages, n_kv_heads, page_size, head_dim / 2], canonical nibbles, 16-byte aligned;
- *   k_scale, v_scale  group = 0: static steps, fp32 [n_kv_heads], finite and positive (not checked: they live on the device);
+ *   k_scale, v_scale  group = 0: static steps, fp32 [n_kv_heads], from 2^-64 to 2^64 (not checked: they live on the device);
  *                     group = 32, 64 or 128 (at most head_dim): dynamic steps, fp32 [n_pages, n_kv_heads, page_size, head_dim / group],
  *                     16-byte aligned, written by pq_kv4_append.
  * The struct itself lies on the host and is read during the call. */
@@ -581,8 +581,11 @@ int pq_kv4_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t
  *     group = 0 the head's static step, else step = fp32(clip * max |z| over the group / 7), 1 for a group of zeros, which is
  *     written as well; clip in (0, 1].  The codes are those of this definition in double precision, dynamic ones with the step that is
  *     written: a value's is exact, a key's off by its fp32 path, 2^-20 of the head vector's length / 7 and 2^-20 of itself at most.
- * Tokens whose slot lies outside the cache (-1 of a padded step) are neither read nor written, in the cache and in q_out.  Two tokens with the
- * same slot leave the codes of either, channel by channel.  n_heads is a multiple of n_kv_heads; T < 2^25, T * (n_heads + 2 n_kv_heads) < 2^31.
+ * Of tokens whose slot lies outside the cache (-1 of a padded step) nothing is written, in the cache or in q_out; their rows of qkv may be read,
+ * and what they hold affects nothing.  A value that is not a number has no code; others of its vector keep theirs where they do not meet it
+ * (in the norm, a pair of the position rotation, the Hadamard rotation, a dynamic step).  Two tokens with the
+ * same slot leave the codes of either, channel by channel.  n_heads is a multiple of n_kv_heads; T < 2^25, n_heads + 2 n_kv_heads < 2^16, their
+ * product < 2^31.
  */
 int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* positions, const int64_t* slots,
                   const void* q_weight_f16, const void* k_weight_f16, float eps, const float* cos_sin, int64_t max_positions,
@@ -603,7 +606,7 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
  * max_q     the most queries of a request: (>= 1) a hint that chooses between kernels: any value is right, and changes results in the order of sums alone.
  * prefix_k, prefix_v  in fp16 [n_prefix, n_kv_heads, head_dim] (rotated like the keys), NULL iff n_prefix = 0; n_prefix <= 1024.
  * out_f16   out [T, n_heads * head_dim] fp16; rows outside [cu_q[0], cu_q[B]) are left as they were; may not lie over q.
- * Scores, sums and the softmax's statistics are fp32; the probabilities are rounded to fp16 for the second product, and the sum that divides
+ * Scores (below 2^20 in size, where fp32 still tells steps of 1/8), sums and the softmax's statistics are fp32; the probabilities are rounded to fp16 for the second product, and the sum that divides
  * it is theirs; with dynamic steps the probabilities times the values' steps are, once for every group, and the sum is of the probabilities
  * before.  A dynamic step that is not finite (append writes one for an infinite value) reaches the queries that see its token, and no others.
  * Sums are taken in an order that depends on the sizes and lengths alone: results are reproducible.

@@ -8,8 +8,8 @@
 //
 // Codes as fp16 operands: u = code + 8 (one exclusive or for eight) moved to bits 4 to 7 of each half is the subnormal number u * 2^-20,
 // which the matrix instructions take exactly: a mask and at most one shift for two codes, no subtraction.  The offset leaves by itself:
-// K (u - 8) q starts its sum at -8 sum(q) 2^-20, and sum p (u - 8) = sum p u - 8 sum p, where sum p is the softmax's own denominator (of
-// the rounded probabilities that the product uses).  (At bits 0 to 3 the products lose low bits against the accumulator: 6e-7 of the largest
+// K (u - 8) q starts its sum at -8 sum(q) 2^-20, and sum p (u - 8) = sum p u - 8 sum p, where sum p is the cached tokens' part of the
+// softmax's own denominator (of the rounded probabilities that the product uses); the prefix tokens' values have no offset.  (At bits 0 to 3 the products lose low bits against the accumulator: 6e-7 of the largest
 // sum, at bits 4 to 7 none were lost.)
 //
 // Probabilities are rounded to fp16 relative to a reference m that lags behind the running maximum: it moves only when a score passes it by
@@ -38,7 +38,7 @@ constexpr int kTileRows = 256;           // rows of a workgroup of the kernel fo
 // 60 | 55; 64 of up to 2000 113 | 137, 146 | 140, 185 | 148; with a step to 32 channels 218 | 307, 284 | 322, 372 | 330.
 constexpr int kSmallRows = 192;
 
-constexpr float kNothing = -1e30f;       // reference before the first score
+constexpr float kNothing = -1e30f;       // reference before the first score (a score is above -2^20)
 constexpr float kMost = 14.0f, kBack = 6.0f;
 constexpr float kUnit = 0x1.0p20f;       // a code as operand is u * 2^-20
 constexpr uint32_t kNibble = 0x00F000F0u, kOffset = 0x88888888u;

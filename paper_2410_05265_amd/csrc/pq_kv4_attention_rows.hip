@@ -27,7 +27,7 @@ __device__ __forceinline__ v4f product(const v8h& a, const v8h& b, const v4f& c)
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kTile = 32;                          // tokens of a wavefront's step: a unit
 constexpr int kDepth = 4;                          // places of a wavefront's ring
-// Two workgroups to a CU: 128 of its 160 KiB of LDS.  (Three with three places, where the registers allow them: 64 requests of up to 8192
+// Two workgroups to a CU: 128 of its 160 KiB of LDS with 128 channels (32 to 40 KiB with 64, where registers would allow three).  (Three with three places, where the registers allow them: 64 requests of up to 8192
 // tokens 84.1 us against 82.4, 24 x 32 heads of up to 2300 42.5 against 43.4, 3 requests of up to 131072 93.8 against 86.4.)
 constexpr int kPerCu = 2, kGroups = 256 * kPerCu;
 constexpr float kLeast = 0x1.0p-80f;               // smallest reference of value weights (dynamic steps)
@@ -132,7 +132,8 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
     const Plan p = plan<ROWS>(a, small_rows, lane);
     // Codes that one wavefront reads once go past the caches, where they would push out each other and, from call to call, themselves: a call's
     // history from 64 MiB on (356 MB 82 -> 73.5 us, 148 MB 43.2 -> 39.8, 342 MB with dynamic steps 84.5 -> 79.9); below, they may be in the
-    // memory-side cache still (27 MB read by each of three calls in turn: 23.4 -> 24.6).
+    // memory-side cache still (27 MB read by each of three calls in turn: 23.4 -> 24.6).  Between 27 and 148 MB nothing was measured, nor
+    // short histories of as many layers as a model has, which the cache does not hold together.
     const bool stream = p.total * (2 * S::CODES) > 64 << 20;
     // (place 0 holds their count; only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
     if (blockIdx.x == 0 && threadIdx.x == 0) items[0].parts = (int)min(p.items, most_items);
@@ -718,8 +719,9 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
     return hip_status(hipGetLastError());
 }
 
-// Column blocks: two where requests have more than 16 rows and the histories of 16 rows are more than 48 units for every wavefront; with less
-// to do, twice the runs of half the work are faster.  One | two, us, 32 heads of 128 on 8: 16 requests of up to 4000 tokens with 32 rows
+// Column blocks: two where requests have more than 16 rows and the histories of 16 rows may be more than 48 units for every wavefront (the host
+// knows the table, not the lengths: under a table far longer than the histories the choice is two); with less to do, twice the runs of half
+// the work are faster.  One | two, us, 32 heads of 128 on 8: 16 requests of up to 4000 tokens with 32 rows
 // (32000 units) 37 | 39, 64 rows 42 | 47, 128 rows (128000) 60 | 57; 64 requests with 20 rows (up to 128000) 55 | 57, 32 rows 69 | 64,
 // 128 rows 190 | 156; one of 131072 with 48 rows (98000) 77 | 69.  Four groups of dynamic steps would not fit the registers twice (16
 // requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).

@@ -6,8 +6,8 @@
 // keys by four wavefronts and values by the other four (the expansion by every wavefront for itself would be eight times the vector
 // instructions, which are scarce beside the exponentials), while the codes after next are on their way.  Two wavefronts share a SIMD: one's
 // exponentials run beside the other's products.  (Four wavefronts of 64 columns with 512 registers each needed fewer reads of LDS and spilled:
-// 1.8 times as long.)  500 queries over 33000 tokens, 64 heads on 8: 537 GFLOP in 520 us, 1030 TFLOP/s (a library product of fp16 matrices:
-// 1171), matrix pipe busy 48 % of the cycles at 2.0 GHz.  4 prompts of up to 4096 tokens, 32 heads on 8: 314 GFLOP in 367 us, 860 TFLOP/s:
+// 1.8 times as long.)  500 queries over 33000 tokens, 64 heads on 8: 537 GFLOP in 510 us, 1050 TFLOP/s (a library product of fp16 matrices:
+// 1171), matrix pipe busy 48 % of the cycles at 2.0 GHz.  4 prompts of up to 4096 tokens, 32 heads on 8: 314 GFLOP in 363 us, 870 TFLOP/s:
 // a workgroup's start and end take as long as five of its steps, of which it has 26 on average, and 5 % of the products meet the mask.
 //
 // Where a call has few tiles of rows, the histories are cut into `splits` parts; their sums go through scratch memory and a second kernel.
@@ -152,8 +152,8 @@ struct Lds {
 };
 
 // Two workgroups to a CU where 128 registers do: one's start and end, and its waits at the barriers, beside the other's products (64 channels,
-// static steps, one | two: 4 prompts of up to 4096 tokens 296 | 252 us, 300 queries each over up to 4000 83 | 75, 500 over 33000 240 | 243;
-// with dynamic steps what does not fit is spilled: 409 | 764).
+// static steps, 32 heads on 8, one | two: 4 prompts of up to 4096 tokens 231 | 203 us, 4 of 4096 385 | 365, 300 queries each over up to 4000 64 |
+// 65, 500 over 33000 177 | 180; with dynamic steps what does not fit is spilled: to 64 channels 347 | 422, 500 over 33000 277 | 531).
 template <int D, int G, bool DYNAMIC>
 __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs a, float* partial, const int32_t* __restrict__ starts, int splits, int small_rows)
 {

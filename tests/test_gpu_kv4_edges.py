@@ -188,6 +188,42 @@ def test_prefix_values_far_smaller_than_the_steps(pq, D, group, q_len, B):
     assert err.max() <= bound
 
 
+@pytest.mark.parametrize("q_len", [1, 60])
+@pytest.mark.parametrize("prefix", [0, 3])
+def test_ends_of_the_static_steps(pq, q_len, prefix):
+    """Steps of 2^-64 and 2^64: codes, attention with all weights alike; scores up to 2^20, where one token has all the weight."""
+    least, most = 2.0 ** -64, 2.0 ** 64
+    a = append_case(30, 4, 2, 64, 1, 0)
+    for step, want in ((least, lambda x: np.clip(np.sign(x) * 8, -8, 7)), (most, lambda x: 0 * x)):
+        a["ks"][:] = a["vs"][:] = step
+        t = [dev(a[n]) for n in ("kc", "vc", "ks", "vs")]
+        pq.pq_kv4_append(dev(a["qkv"]), 4, None, dev(a["slots"]), *t, rotate=False)
+        x = a["qkv"].astype(np.float64).reshape(30, 8, 64)
+        for codes, y in ((t[0], x[:, 4:6]), (t[1], x[:, 6:])):
+            assert np.array_equal(R.unpack(host(codes)[a["slots"] // 16, :, a["slots"] % 16]), want(y))
+    c = attention_case([200, 90], [q_len, q_len], 8, 2, 64, 2, 0, 16, prefix=prefix)
+    c["ks"][:] = least
+    if prefix:
+        c["pk"][:] = 0
+    for step in (least, 2.0 ** 10):
+        c["vs"][:] = step
+        check_cut(pq, c, hints=(q_len,))
+    # the largest score of the cached tokens decides: the next is further off than fp32 could mistake
+    c["ks"][:], c["vs"][:] = 2.0 ** 14, 1.0
+    got = host(call(pq, put(c), q_len)).reshape(-1, 8, 64)
+    cu, table = c["cu"], c["table"]
+    for b, n in enumerate((200, 90)):
+        for h in range(2):
+            k, v = (R.unpack(x[table[b, :-(-n // 16)], h]).reshape(-1, 64)[:n].astype(np.float64) for x in (c["kc"], c["vc"]))
+            for i in range(q_len):
+                for g in range(4 * h, 4 * h + 4):
+                    s = (k @ c["q"][cu[b] + i, 64 * g:64 * g + 64].astype(np.float64))[:n - (q_len - 1 - i)]
+                    assert np.abs(s).max() * 0.125 * 2 ** 14 < 2 ** 20
+                    one, two = np.sort(s)[[-1, -2]]
+                    if one - two > 2e-4 * np.abs(s).max() and (one > 1 or not prefix):   # (e^-50 and less for the others)
+                        assert np.array_equal(got[cu[b] + i, g], v[np.argmax(s)])
+
+
 # ------------------------------------------------------------------------------------------------ very many requests
 @pytest.mark.parametrize("B,q,short", [(32768, 3, 0), (32769, 3, 0), (40001, 5, 20000), (100003, 4, 0), (131072, 2, 100000)])
 def test_slots_of_more_requests_than_workgroups(pq, B, q, short):
