@@ -608,7 +608,7 @@ int pq_kv4_append(const void* qkv_f16, int64_t row_stride, int64_t T, int32_t n_
  * out_f16   out [T, n_heads * head_dim] fp16; rows outside [cu_q[0], cu_q[B]) are left as they were; may not lie over q.
  * Scores (below 2^20 in size, where fp32 still tells steps of 1/8), sums and the softmax's statistics are fp32; the probabilities are rounded to fp16 for the second product, and the sum that divides
  * it is theirs; with dynamic steps the probabilities times the values' steps are, once for every group, and the sum is of the probabilities
- * before.  A dynamic step that is not finite (append writes one for an infinite value) reaches the queries that see its token, and no others.
+ * before.  A request of up to 32 rows (queries times n_heads / n_kv_heads) has those that are a large part of a sum in 22 bits instead of 11.  A dynamic step that is not finite (append writes one for an infinite value) reaches the queries that see its token, and no others.
  * Sums are taken in an order that depends on the sizes and lengths alone: results are reproducible.
  * workspace: device memory, 256-byte aligned, pq_kv4_attention_workspace_bytes of the same arguments (at most 160 MiB, and 2 bytes for each
  *     of T * n_heads + 16 * B * n_kv_heads; 0 for sizes that the call refuses).  What it holds need not be set, and calls that may run at

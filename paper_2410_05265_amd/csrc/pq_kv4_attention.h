@@ -17,7 +17,9 @@
 // rescaled only when the reference moves, by a power of two, and the denominator sums what was rounded: where one token has all the weight its
 // rounding leaves again.  With dynamic steps the product takes weights p * step, rounded once, a rounding for every group of channels; the
 // denominator then sums p as it is: the sum of rounded p would be a second, independent error, sqrt(3) instead of sqrt(2) times the rounding of
-// the fp16 result where one token has the weight (measured over histories of 1 to 2000 tokens: 1.40 to 1.45, static steps 1.0 to 1.44).
+// the fp16 result where one token has the weight (measured over histories of 1 to 2000 tokens: 1.40 to 1.45, static steps 1.0 to 1.44).  That is
+// over many rows; where a call has few of them these errors do not average out, and the kernel for few rows takes large weights as two fp16
+// numbers each.
 #pragma once
 
 #include "pq_kv4.h"

@@ -224,6 +224,46 @@ def test_ends_of_the_static_steps(pq, q_len, prefix):
                         assert np.array_equal(got[cu[b] + i, g], v[np.argmax(s)])
 
 
+# ------------------------------------------------------------------------------------------------ roundings of the weights
+def check_result_is_rounded_once(pq, c, q_len):
+    """Within half a step of fp16 of the exact result, and 2^-18 of the values (weights of 22 bits, twice; sums and scores in fp32)."""
+    want, _, real = R.attention(c["q"], c["cu"], c["kv"], c["table"], c["kc"], c["vc"], c["ks"], c["vs"], c["scale"], c["group"], c["pk"], c["pv"])
+    got = host(call(pq, put(c), q_len)).astype(np.float64).reshape(want.shape)
+    # (a value is at most 8 * 0.6; sums with the codes' offset 15 + 8 of them, rounded a few times to 2^-24)
+    assert np.all((np.abs(got - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -18 * 8 * 0.6 + 2.0 ** -25)[real])
+
+
+@pytest.mark.parametrize("D,group", [(64, 0), (64, 32), (64, 64), (128, 0), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("prefix", [0, 3])
+def test_short_histories_are_rounded_once(pq, D, group, prefix):
+    """Histories of one tile: every weight is a large one.  Scores of a few units, off by 2^-20: 2^-19 of a value at most, in the bound above."""
+    n = np.arange(1, 33)
+    check_result_is_rounded_once(pq, attention_case(n, [1] * 32, 4, 2, D, 5, group, 16, prefix=prefix, q_size=0.2), 1)
+
+
+@pytest.mark.parametrize("D,group", [(64, 0), (64, 32), (64, 64), (128, 0), (128, 32), (128, 64), (128, 128)])
+@pytest.mark.parametrize("q_len", [1, 3])
+def test_one_token_with_all_the_weight_is_rounded_once(pq, D, group, q_len):
+    """Somewhere in a long history; the others have less than 2^-25 of a value together."""
+    kv = [3000, 700, 61, 1500]
+    c = attention_case(kv, [q_len] * 4, 4, 2, D, 6, group, 16, q_size=0.3)
+    r = np.random.default_rng(8)
+    q = c["q"].reshape(-1, 4, D)
+    sign = np.where(r.random((4, 2, D)) < 0.5, -1.0, 1.0)          # of each request and key/value head
+    for b, n in enumerate(kv):
+        lo = int(c["cu"][b])
+        for h in range(2):
+            q[lo:lo + q_len, 2 * h:2 * h + 2] = np.abs(q[lo:lo + q_len, 2 * h:2 * h + 2]) * sign[b, h] + 2.0 * sign[b, h]
+            t = int(r.integers(0, n - q_len))
+            page = c["table"][b, t // 16]
+            c["kc"][page, h, t % 16] = R.pack(7 * sign[b, h])
+            if group:
+                c["ks"][page, h, t % 16] = 0.6
+            else:
+                c["ks"][:] = 0.6
+    check_result_is_rounded_once(pq, c, q_len)
+
+
 # ------------------------------------------------------------------------------------------------ very many requests
 @pytest.mark.parametrize("B,q,short", [(32768, 3, 0), (32769, 3, 0), (40001, 5, 20000), (100003, 4, 0), (131072, 2, 100000)])
 def test_slots_of_more_requests_than_workgroups(pq, B, q, short):
