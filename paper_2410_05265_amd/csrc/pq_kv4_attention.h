@@ -35,9 +35,11 @@ typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kTileRows = 256;           // rows of a workgroup of the kernel for many queries
 
-// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and the others the row kernel.  Row | tile kernel, us,
-// 32 heads of 128 on 8: one request of 33000 tokens with 128 rows 56 | 107, 192 63 | 110, 256 77 | 79; 8 of up to 4000 46 | 63, 52 | 54,
-// 60 | 55; 64 of up to 2000 113 | 137, 146 | 140, 185 | 148; with a step to 32 channels 218 | 307, 284 | 322, 372 | 330.
+// Where a call may hold requests of more rows than kSmallRows, those take the tile kernel and the others the row kernel.  Row | tile kernel
+// alone, us, 32 heads of 128 on 8, with 128, 192 and 256 rows: one request of 33000 tokens 62 | 73, 62 | 72, 75 | 73; 8 of 2000 to 4000 51 | 59,
+// 57 | 47, 69 | 49; 64 of 1000 to 2000 139 | 129, 177 | 122, 221 | 126, with a step to 32 channels 261 | 262, 373 | 264, 485 | 266.  (Of several
+// requests the row kernel is launched for the others as well, 8 us; many requests of 129 to 192 rows would gain from a lower border all the
+// same, a single one would lose.)
 constexpr int kSmallRows = 192;
 
 constexpr float kNothing = -1e30f;       // reference before the first score (a score is above -2^20)

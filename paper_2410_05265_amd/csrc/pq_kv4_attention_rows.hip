@@ -766,10 +766,10 @@ int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
 
 // Column blocks: two where requests have more than 16 rows and the histories of 16 rows may be more than 48 units for every wavefront (the host
 // knows the table, not the lengths: under a table far longer than the histories the choice is two); with less to do, twice the runs of half
-// the work are faster.  One | two, us, 32 heads of 128 on 8: 16 requests of up to 4000 tokens with 32 rows
-// (32000 units) 37 | 39, 64 rows 42 | 47, 128 rows (128000) 60 | 57; 64 requests with 20 rows (up to 128000) 55 | 57, 32 rows 69 | 64,
-// 128 rows 190 | 156; one of 131072 with 48 rows (98000) 77 | 69.  Four groups of dynamic steps would not fit the registers twice (16
-// requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
+// the work are faster.  One | two, us, 32 heads of 128 on 8: 16 requests of 2000 to 4000 tokens with 20 rows 36 | 34, 32 rows (32000 units) 37 |
+// 40, 64 rows 50 | 48, 128 rows (128000) 78 | 66; 64 requests with 20 rows (up to 128000) 81 | 66, 32 rows 84 | 78, 128 rows 261 | 197; one of
+// 131072 with 48 rows (98000) 85 | 75; one step to a head, 64 requests, 128 rows 297 | 229.  Four groups of dynamic steps would not fit the
+// registers twice (16 requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
 int blocks_for(int32_t max_q, int32_t per_kv, int64_t units) { return (int64_t)max_q * per_kv > 16 && units > 48 * kGroups * kWaves ? 2 : 1; }
 
 bool takes_tiles(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv > kSmallRows; }
