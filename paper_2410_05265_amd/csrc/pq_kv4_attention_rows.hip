@@ -2,7 +2,7 @@
 //
 // The queries of a request that share a key/value head (its tokens times the heads of the group) are the columns of the matrix instructions,
 // 16 or 32 of them (CB blocks of 16), so that up to as many read every code once.  Bound by HBM: 128 bytes of codes for a token and head of
-// 128 channels.  One token each of 64 requests of up to 8192 cached ones, 32 heads on 8: 356 MB in 70 us and 4 for the second kernel, where
+// 128 channels.  One token each of 64 requests of up to 8192 cached ones, 32 heads on 8: 356 MB in 72 us and 4.6 for the second kernel, where
 // a kernel that only reads as many bytes in a row takes 56.  One request of 1537 tokens: 7 us and 4, all latency.
 //
 // Work is cut over the histories, in units of kTile tokens of one request, head and tile of rows.  All units of the call lie one after another,
