@@ -146,8 +146,8 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
     const Plan p = plan<ROWS>(a, small_rows, lane);
     // Codes that one wavefront reads once go past the caches, where they would push out each other and, from call to call, themselves: a call's
     // history from 64 MiB on (356 MB 82 -> 73.5 us, 148 MB 43.2 -> 39.8, 342 MB with dynamic steps 84.5 -> 79.9); below, they may be in the
-    // memory-side cache still (27 MB read by each of three calls in turn: 23.4 -> 24.6).  Between 27 and 148 MB nothing was measured, nor
-    // short histories of as many layers as a model has, which the cache does not hold together.
+    // memory-side cache still, where a program has few caches: three in turn, through the caches | past them, 32 MB 18.5 | 19.1, 59 MB 26.5 |
+    // 27.8, and 27 MB with dynamic steps 23.4 | 24.6; thirty-two in turn 16 MB 16.3 | 15.9, 32 MB 20.0 | 19.4, 59 MB 28.4 | 27.9.
     const bool stream = p.total * (2 * S::CODES) > 64 << 20;
     // (place 0 holds their count; only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
     if (blockIdx.x == 0 && threadIdx.x == 0) items[0].parts = (int)min(p.items, most_items);
