@@ -12,10 +12,11 @@
 //
 // Bound by HBM: 2 bytes of every channel in, 2 out for queries and half a byte for keys and values (8192 tokens x 48 heads of 128: 180 MB in
 // 44 us, 4.1 TB/s, where a copy of as many bytes takes 35); with norms and dynamic steps (2111 tokens x 80 heads: 81 MB in 26 us) by no one
-// thing: vector instructions issue in 39 % of the cycles, and the wavefronts are a round and a fifth of what the card holds; a step of 64 tokens by its launch and three dependent loads (4.5 us).  A lane holds eight channels
-// (16 bytes), D / 8 lanes a head, a wavefront the same head of 8 or 4 consecutive tokens: one kind of work to a wavefront, the step and
-// the norm's weights are read once, and in a page the tokens of a head lie one after another.  The four wavefronts of a workgroup take
-// four neighbouring heads of these tokens, which share the rows of the table of angles.
+// thing: vector instructions issue in 39 % of the cycles, and the wavefronts are a round and a fifth of what the card holds; a step of 64
+// tokens by its launch and three dependent loads (4.5 us).  A lane holds eight channels (16 bytes), D / 8 lanes a head, a wavefront the same
+// head of 8 or 4 consecutive tokens: one kind of work to a wavefront, the step and the norm's weights are read once, and in a page the tokens
+// of a head lie one after another.  The four wavefronts of a workgroup take four neighbouring heads of these tokens, which share the rows of
+// the table of angles.
 #include "pq_kv4.h"
 #include "pq_rotate.h"
 
