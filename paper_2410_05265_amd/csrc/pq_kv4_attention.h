@@ -9,7 +9,9 @@
 // Codes as fp16 operands: u = code + 8 (one exclusive or for eight) moved to bits 4 to 7 of each half is the subnormal number u * 2^-20,
 // which the matrix instructions take exactly: a mask and at most one shift for two codes, no subtraction.  The offset leaves by itself:
 // K (u - 8) q starts its sum at -8 sum(q) 2^-20, and sum p (u - 8) = sum p u - 8 sum p, where sum p is the cached tokens' part of the
-// softmax's own denominator (of the rounded probabilities that the product uses); the prefix tokens' values have no offset.  (At bits 0 to 3 the products lose low bits against the accumulator: 6e-7 of the largest
+// softmax's own denominator (of the rounded probabilities that the product uses); the prefix tokens' values have no offset.  Over n
+// tokens of like weight the sum with the offset is some 2 sqrt(n) times the one without, and its roundings as many times larger, so the
+// kernel for few rows takes it off every 64 tiles, and the one for many rows has values without it in its operands.  (At bits 0 to 3 the products lose low bits against the accumulator: 6e-7 of the largest
 // sum, at bits 4 to 7 none were lost.)
 //
 // Probabilities are rounded to fp16 relative to a reference m that lags behind the running maximum: it moves only when a score passes it by
@@ -78,6 +80,8 @@ __device__ __forceinline__ uint32_t two_halves(float a, float b)
     return __builtin_bit_cast(uint32_t, h);
 }
 
+// (Cuts off what `to` has no bits for instead of rounding: over a long history a denominator so added was 2^-24 too small for each addition,
+// 3e-4 after 32768 tokens, and eight times as much in a static step's offset.  So only a tile's own weights are added with it.)
 __device__ __forceinline__ float add_halves(uint32_t pair, float to)
 {
     const v2h one = {(_Float16)1.0f, (_Float16)1.0f};

@@ -120,7 +120,8 @@ __device__ __forceinline__ v4u rest_in_halves(const float (&w)[8])
     for (int i = 0; i < 8; ++i) rest[i] = w[i] - (float)(_Float16)w[i];
     return in_halves(rest);
 }
-__device__ __forceinline__ float add_eight(const v4u& w, float to) { return add_halves(w[3], add_halves(w[2], add_halves(w[1], add_halves(w[0], to)))); }
+// (Their own sum first: add_halves.)
+__device__ __forceinline__ float add_eight(const v4u& w, float to) { return to + add_halves(w[3], add_halves(w[2], add_halves(w[1], add_halves(w[0], 0.0f)))); }
 
 template <int D, int G, bool DYNAMIC, int CB>
 struct Shape {
@@ -292,13 +293,13 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         }
 
         float m[CB], l[CB];                        // l: of this lane's tokens
-        float l_prefix[CB];                        // static steps: of the prefix tokens, whose values have no offset
+        float l_free[CB];                          // static steps: of tokens whose values' offset is not in o (prefix), or no longer
         v4f o[CB][NG * CH];
         float ref[CB][NG], lw[CB][NG];             // dynamic steps: weights p * step are rounded relative to ref
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             m[c] = kNothing;
-            l[c] = l_prefix[c] = 0.0f;
+            l[c] = l_free[c] = 0.0f;
 #pragma unroll
             for (int i = 0; i < NG * CH; ++i) o[c][i] = (v4f){0, 0, 0, 0};
 #pragma unroll
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                         for (int i = 0; i < CH; ++i) o[c][g * CH + i] *= f;
                     }
                 } else {
-                    l_prefix[c] *= alpha;
+                    l_free[c] *= alpha;
 #pragma unroll
                     for (int i = 0; i < NG * CH; ++i) o[c][i] *= alpha;
                 }
@@ -407,7 +408,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 #pragma unroll
                 for (int g = 0; g < NG; ++g) ref[c][g] = kLeast;
                 if constexpr (!DYNAMIC) {
-                    l_prefix[c] = l[c];
+                    l_free[c] = l[c];
                     l[c] = 0.0f;
                 }
             }
@@ -597,6 +598,23 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
                     products(rest);
                 }
             }
+            // The codes' offset is taken off every 64 tiles: over n tokens of like weight it is some 2 sqrt(n) times the values' sum, and its
+            // roundings would pass the result's own after a few thousand tokens in a row.
+            if (i % 64 == 63) {
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        float& sum = DYNAMIC ? lw[c][g] : l[c];
+                        float all = sum + __shfl_xor(sum, 16, 64);
+                        all += __shfl_xor(all, 32, 64);
+                        all *= 8.0f / kUnit;
+#pragma unroll
+                        for (int j = 0; j < CH; ++j) o[c][g * CH + j] -= all;
+                        if constexpr (!DYNAMIC) l_free[c] += sum;
+                        sum = 0.0f;
+                    }
+            }
         }
 
         // ---- results.  Block j of a group holds channels CH * row + j: a lane's rows 4 quarter .. + 3 are 4 CH channels in a row.
@@ -606,8 +624,8 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             l[c] += __shfl_xor(l[c], 32, 64);
             float l_all = l[c];
             if constexpr (!DYNAMIC) {
-                l_prefix[c] += __shfl_xor(l_prefix[c], 16, 64);
-                l_all += l_prefix[c] + __shfl_xor(l_prefix[c], 32, 64);
+                l_free[c] += __shfl_xor(l_free[c], 16, 64);
+                l_all += l_free[c] + __shfl_xor(l_free[c], 32, 64);
             }
             const int row = tile * ROWS + 16 * c + col;
             const bool live = row < rows;

@@ -264,6 +264,42 @@ def test_one_token_with_all_the_weight_is_rounded_once(pq, D, group, q_len):
     check_result_is_rounded_once(pq, c, q_len)
 
 
+# ------------------------------------------------------------------------------------------------ sums over long flat histories
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("many", [False, True])
+def test_means_over_long_histories(pq, group, many):
+    """Weights all alike and without a rounding of their own (static steps: it stands above and below the fraction; dynamic ones: the weight is the
+    step, of 11 bits, times a power of two), and no round numbers: the sums have to round.  The result is the mean of the values, 4.3 / sqrt(n) of
+    a code: far below the offset of 8 that codes may have on their way, whose sums of up to 8 n codes, rounded to half of 2^-24, n / 16 times in a
+    row at random, are off by 2^-25 * 8 n * sqrt(n / 16 / 3): 5 % of the result's own rounding (2^-12 of it) for n = 2000 tokens in a row, nine times
+    it for 32768.  A denominator that is cut off instead of rounded, 2^-24 of it for each of n / 4 pairs of a lane, is 2^-24 * n / 8 too small: 2^-12 for
+    n = 32768.  Right sums leave the result's rounding alone, plus next to nothing."""
+    Hq, Hkv, D, ps, W = 32, 8, 128, 1024, 128
+    r = np.random.default_rng(9)
+    kc, vc = (R.pack(r.integers(-7, 8, (W, Hkv, ps, D))) for _ in range(2))
+    shape = (W, Hkv, ps, 1) if group else (Hkv,)
+    step = 0.5 * (1 + 683 / 1024)
+    ks, vs = (np.full(shape, step, np.float32) for _ in range(2))
+    kc[..., 0] = 0x33                                              # channels 0 and 1 of every key: 3
+    if many:                                                       # one request of many rows
+        B, kv, q_len = 1, np.array([W * ps - 5]), 1024
+    else:                                                          # decoded tokens of many requests, over the same pages
+        B, q_len = 192, 1
+        kv = W * ps - 1 - 9 * np.arange(B)
+    table = np.broadcast_to(r.permutation(W).astype(np.int32), (B, W)).copy()
+    q = torch.zeros((B * q_len, Hq * D), dtype=torch.float16, device="cuda")
+    if not group:
+        q.view(-1, Hq, D)[:, :, 0] = 1.7
+    out, _ = pq.pq_kv4_attention(q, i32(np.arange(B + 1) * q_len), i32(kv), dev(table), dev(kc), dev(vc), dev(ks), dev(vs), D ** -0.5, q_len, group=group)
+    code = R.unpack(vc[table[0]].transpose(0, 2, 1, 3).reshape(W * ps, Hkv, D // 2)).astype(np.int64)
+    total = np.cumsum(code, axis=0)
+    n = (kv[:, None] - (q_len - 1 - np.arange(q_len))).reshape(-1)
+    want = np.repeat(step * total[n - 1] / n[:, None, None], Hq // Hkv, axis=1)
+    err = host(out).astype(np.float64).reshape(want.shape) - want
+    rounding = want.astype(np.float16).astype(np.float64) - want
+    assert np.sqrt((err ** 2).mean()) <= 1.05 * np.sqrt((rounding ** 2).mean())
+
+
 # ------------------------------------------------------------------------------------------------ very many requests
 @pytest.mark.parametrize("B,q,short", [(32768, 3, 0), (32769, 3, 0), (40001, 5, 20000), (100003, 4, 0), (131072, 2, 100000)])
 def test_slots_of_more_requests_than_workgroups(pq, B, q, short):
