@@ -154,8 +154,8 @@ struct Lds {
 };
 
 // Two workgroups to a CU where 128 registers do: one's start and end, and its waits at the barriers, beside the other's products (64 channels,
-// static steps, 32 heads on 8, one | two: 4 prompts of up to 4096 tokens 231 | 203 us, 4 of 4096 385 | 365, 300 queries each over up to 4000 64 |
-// 65, 500 over 33000 177 | 180; with dynamic steps what does not fit is spilled: to 64 channels 347 | 422, 500 over 33000 277 | 531).
+// static steps, 32 heads on 8, one | two: 4 prompts of up to 4096 tokens 232 | 206 us, 4 of 4096 390 | 357, 300 queries each over up to 4000 64 |
+// 65, 500 over 33000 178 | 184; with dynamic steps what does not fit is spilled: to 64 channels 347 | 422, 500 over 33000 277 | 531).
 template <int D, int G, bool DYNAMIC>
 __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs a, float* partial, const int32_t* __restrict__ starts, int splits, int small_rows)
 {
