@@ -622,6 +622,68 @@ int pq_kv4_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n
                      const void* prefix_k_f16, const void* prefix_v_f16, int32_t n_prefix, float softmax_scale, int32_t causal,
                      void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Attention of the same kind with a sliding window and first tokens that stay visible.  Row cu_q[b] + i stands at p = kv_len[b] - q_len + i of its
+ * request and sees the prefix tokens and the cached tokens t <= p with
+ *     t < sinks   or   t > p - window;
+ * everything else is as in pq_kv4_attention with causal != 0.  window >= 1 (any number: one that is as long as the history hides nothing),
+ * sinks >= 0.  Only pages with tokens that a row of the request sees are read, but for the ends of their 64 tokens: entries of the table in between may be
+ * anything, -1 among it, as where a server has taken such pages back.
+ * workspace: pq_kv4_window_attention_workspace_bytes of the same arguments (at most what pq_kv4_attention's says of itself). */
+size_t pq_kv4_window_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, int32_t window,
+                                               int32_t sinks, const pq_kv4_cache* cache);
+int pq_kv4_window_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* cu_q, const int32_t* kv_len,
+                            int32_t B, int32_t max_q, const int32_t* block_table, int32_t table_pages, const pq_kv4_cache* cache,
+                            const void* prefix_k_f16, const void* prefix_v_f16, int32_t n_prefix, float softmax_scale, int32_t window,
+                            int32_t sinks, void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Trees of drafted tokens.  The new tokens of a request, up to 32 * words of them (its rows below T), are the nodes of a tree: row
+ * cu_q[b] + i is node i, cached at c + i with c = kv_len[b] - q_len tokens in front, and parents[cu_q[b] + i] is the number of the node before it in its
+ * branch, less than i; anything else makes it a root.  A request of more rows is a prompt, a chain.
+ *
+ * pq_kv4_tree: masks and positions.
+ *     mask[t, w] bit j: node 32 w + j is node i itself or one of the nodes above it (int32 [T, words]; 0 in the rows of prompts),
+ *     positions[t] = position_offset + c + (nodes above it)          (a prompt's: position_offset + c + i).
+ * Rows of no request, behind the last one up to T, get 0 in both.  They replace the positions that pq_kv4_slots gave, in front of pq_kv4_append.
+ * words: 1 to 8.  Outputs may not lie over inputs (PQ_ERR_UNSUPPORTED).  0 <= B < 2^26, 0 <= T < 2^30. */
+int pq_kv4_tree(const int32_t* parents, const int32_t* cu_q, const int32_t* kv_len, int32_t B, int64_t T, int32_t words, int32_t position_offset,
+                int32_t* mask, int32_t* positions, void* stream);
+
+/* pq_kv4_tree_attention: row i of a tree sees the prefix tokens, the nodes j < q_len of its mask (any mask: a node need not see itself) at c + j,
+ * and the tokens t < c with
+ *     t < sinks   or   t >= c + (nodes that it sees) - window;
+ * rows of prompts see what pq_kv4_window_attention says.  window = 0: no window.  A row that sees nothing gets zeros.  Everything else, the
+ * workspace's size with it, is as in pq_kv4_window_attention. */
+size_t pq_kv4_tree_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, int32_t window,
+                                             int32_t sinks, const pq_kv4_cache* cache);
+int pq_kv4_tree_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* cu_q, const int32_t* kv_len,
+                          int32_t B, int32_t max_q, const int32_t* block_table, int32_t table_pages, const pq_kv4_cache* cache,
+                          const void* prefix_k_f16, const void* prefix_v_f16, int32_t n_prefix, float softmax_scale, const int32_t* mask,
+                          int32_t words, int32_t window, int32_t sinks, void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+
+/* pq_kv4_accept: what of the trees stays, after the model has chosen the token behind every row (chosen, int32 [T]; tokens: the drafted ones, int32 [T]).
+ * Node 0 of a tree, the token that the last step chose, stays; behind a node that stays, the first child (of the lowest number, a child standing
+ * behind its parent) whose token is the one chosen at that node, until there is none or `depth` nodes stay.  Of a prompt all rows stay.
+ *     accepted[b]: how many stay;  next_token[b]: chosen at the last of them, -1 without rows;  kv_len_out[b] = c + accepted[b];
+ *     path[b, k] (int32 [B, depth]): the k-th node that stays, -1 behind them and in prompts;
+ *     from_slots, to_slots [b, k] (int64 [B, depth], 8-byte aligned): the slots of c + path[b, k] and of c + k, where the codes have to go; -1 where
+ *         they are there already, or no page holds one of them;
+ *     free_pages, n_free, taken: pq_kv4_slots' list, and how much of it is given out.  The pages of the columns
+ *         ceil(kv_len_out[b] / page_size) ... ceil(kv_len[b] / page_size) - 1 go back (entries of -1 are none): with r of them, request after request, and
+ *         top = min(taken, n_free), the k-th goes to free_pages[top - 1 - k], and taken_out[0] = top - r (where more come than were given out, what is
+ *         too many stays out of the list, and it is 0).  block_table itself stays: pq_kv4_slots writes these columns anew.  n_free = 0: no list, taken_out[0] = 0.
+ * Outputs may not lie over inputs.  1 <= depth <= 32 * words. */
+int pq_kv4_accept(const int32_t* tokens, const int32_t* parents, const int32_t* chosen, const int32_t* cu_q, const int32_t* kv_len, int32_t B,
+                  int64_t T, int32_t words, int32_t depth, const int32_t* block_table, int32_t table_pages, int32_t page_size,
+                  int32_t* free_pages, int32_t n_free, const int32_t* taken, int32_t* accepted, int32_t* next_token, int32_t* path,
+                  int32_t* kv_len_out, int64_t* from_slots, int64_t* to_slots, int32_t* taken_out, void* stream);
+
+/* pq_kv4_keep: the codes (and dynamic steps) of slot from_slots[b, k] go to slot to_slots[b, k], of every head, in every layer: caches, n_caches of
+ * them on the host, of the same sizes.  Entries with a slot outside the cache move nothing.  In a row b, entry k may write where an earlier entry (or it
+ * itself) reads, as pq_kv4_accept's do; one that writes where a later one, or another row's, reads or writes leaves one or the other there.
+ * 1 <= width <= 256;  B < 2^26, B * n_kv_heads < 2^30. */
+int pq_kv4_keep(const int64_t* from_slots, const int64_t* to_slots, int32_t B, int32_t width, const pq_kv4_cache* caches, int32_t n_caches,
+                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

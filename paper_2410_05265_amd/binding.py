@@ -103,6 +103,16 @@ SIGNATURES = {
     "pq_kv4_attention_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32, _cache]),
     "pq_kv4_attention": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _cache, _vp, _vp, _i32, _f32, _i32, _vp, _vp,
                                         _sz, _vp]),
+    "pq_kv4_window_attention_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _cache]),
+    "pq_kv4_window_attention": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _cache, _vp, _vp, _i32, _f32, _i32, _i32,
+                                               _vp, _vp, _sz, _vp]),
+    "pq_kv4_tree": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _vp]),
+    "pq_kv4_tree_attention_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _cache]),
+    "pq_kv4_tree_attention": (ctypes.c_int, [_vp, _i64, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _cache, _vp, _vp, _i32, _f32, _vp, _i32,
+                                             _i32, _i32, _vp, _vp, _sz, _vp]),
+    "pq_kv4_accept": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                     _vp, _vp, _vp]),
+    "pq_kv4_keep": (ctypes.c_int, [_vp, _vp, _i32, _i32, _cache, _i32, _vp]),
 }
 
 
@@ -114,7 +124,7 @@ class _Declines:
     def linear(*args):
         return -1
 
-    linear2 = kv4_slots = kv4_append = kv4_attention = linear
+    linear2 = kv4_slots = kv4_append = kv4_attention = kv4_window_attention = kv4_tree = kv4_tree_attention = kv4_accept = kv4_keep = linear
 
 
 _lib = None
@@ -138,6 +148,8 @@ def _load_call(L):
         return _Declines
     call.bind(*(ctypes.cast(getattr(L, f), _vp).value for f in ("pq_linear", "pq_linear2")))
     call.bind_kv4(*(ctypes.cast(getattr(L, f), _vp).value for f in ("pq_kv4_slots", "pq_kv4_append", "pq_kv4_attention")))
+    call.bind_kv4_more(*(ctypes.cast(getattr(L, f), _vp).value for f in ("pq_kv4_window_attention", "pq_kv4_tree", "pq_kv4_tree_attention",
+                                                                          "pq_kv4_accept", "pq_kv4_keep")))
     return call
 
 
@@ -796,27 +808,14 @@ def pq_kv4_append(qkv, n_heads: int, positions, slots, k_codes, v_codes, k_scale
     return out
 
 
-def pq_kv4_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, k_codes) -> int:
-    """Scratch memory of pq_kv4_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
+def _kv4_sizes(k_codes):
+    """A cache's sizes, for a workspace query."""
     n_pages, heads, page_size, half = k_codes.shape
-    cache = KV4Cache(None, None, None, None, n_pages, heads, 2 * half, page_size, 0)
-    return int(lib().pq_kv4_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), cache))
+    return KV4Cache(None, None, None, None, n_pages, heads, 2 * half, page_size, 0)
 
 
-def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, group: int = 0,
-                     prefix_k=None, prefix_v=None, causal: bool = True, out=None, workspace=None):
-    """Attention of q fp16 [T, n_heads * head_dim] over the cache behind optional prefix tokens (fp16 [n, kv heads, head_dim]): rows
-    cu_q[b] .. cu_q[b + 1] are request b's, whose kv_len[b] tokens lie in the pages block_table[b].  Returns (out, workspace)."""
-    if out is not None and workspace is not None:
-        if _lib is None:
-            lib()
-        rc = _call.kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k, prefix_v,
-                                 causal, out, workspace)
-        if rc == PQ_OK:
-            return out, workspace
-        if rc > 0:
-            raise PQError(rc, "pq_kv4_attention")
-    cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
+def _kv4_attend(name, q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v, sight, sizes, out, workspace):
+    """One of the three attentions, argument checks and call; sight: its arguments behind softmax_scale, sizes: those of its workspace query."""
     _rows(q, "q")
     _here(cu_q, torch.int32, "cu_q")
     _here(kv_len, torch.int32, "kv_len")
@@ -835,7 +834,7 @@ def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_
                 raise ValueError("shape mismatch")
     W = block_table.shape[1]
     if workspace is None:
-        need = int(lib().pq_kv4_attention_workspace_bytes(T, B, n_heads, int(max_q), W, cache))
+        need = int(getattr(lib(), name + "_workspace_bytes")(T, B, n_heads, int(max_q), W, *sizes, cache))
         workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=q.device)
     else:
         _here(workspace, torch.uint8, "workspace")
@@ -844,10 +843,190 @@ def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_
     else:
         _here(out, torch.float16, "out")
         _result(out, T * n_heads * D, "out")
-    _check(lib().pq_kv4_attention(_ptr(q), q.stride(0) if T > 1 else q.shape[1], T, n_heads, _ptr(cu_q), _ptr(kv_len), B, int(max_q),
-                                  _ptr(block_table), W, cache, _ptr(prefix_k), _ptr(prefix_v), n_prefix, float(softmax_scale), int(bool(causal)),
-                                  _ptr(out), _ptr(workspace), workspace.numel(), _stream()), "pq_kv4_attention")
+    _check(getattr(lib(), name)(_ptr(q), q.stride(0) if T > 1 else q.shape[1], T, n_heads, _ptr(cu_q), _ptr(kv_len), B, int(max_q),
+                                _ptr(block_table), W, cache, _ptr(prefix_k), _ptr(prefix_v), n_prefix, float(softmax_scale), *sight,
+                                _ptr(out), _ptr(workspace), workspace.numel(), _stream()), name)
     return out, workspace
+
+
+def pq_kv4_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, k_codes) -> int:
+    """Scratch memory of pq_kv4_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
+    return int(lib().pq_kv4_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), _kv4_sizes(k_codes)))
+
+
+def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, group: int = 0,
+                     prefix_k=None, prefix_v=None, causal: bool = True, out=None, workspace=None):
+    """Attention of q fp16 [T, n_heads * head_dim] over the cache behind optional prefix tokens (fp16 [n, kv heads, head_dim]): rows
+    cu_q[b] .. cu_q[b + 1] are request b's, whose kv_len[b] tokens lie in the pages block_table[b].  Returns (out, workspace)."""
+    if out is not None and workspace is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k, prefix_v,
+                                 causal, out, workspace)
+        if rc == PQ_OK:
+            return out, workspace
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_attention")
+    cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
+    return _kv4_attend("pq_kv4_attention", q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v, (int(bool(causal)),), (),
+                       out, workspace)
+
+
+def pq_kv4_window_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, window: int, sinks: int, k_codes) -> int:
+    """Scratch memory of pq_kv4_window_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
+    return int(lib().pq_kv4_window_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), int(window), int(sinks),
+                                                             _kv4_sizes(k_codes)))
+
+
+def pq_kv4_window_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, window: int,
+                            sinks: int = 0, group: int = 0, prefix_k=None, prefix_v=None, out=None, workspace=None):
+    """pq_kv4_attention, causal, where a row sees the last `window` tokens up to its own and the first `sinks` ones.  Returns (out, workspace)."""
+    if out is not None and workspace is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_window_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k,
+                                        prefix_v, window, sinks, out, workspace)
+        if rc == PQ_OK:
+            return out, workspace
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_window_attention")
+    cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
+    sight = (int(window), int(sinks))
+    return _kv4_attend("pq_kv4_window_attention", q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v, sight, sight,
+                       out, workspace)
+
+
+def pq_kv4_tree(parents, cu_q, kv_len, words: int, position_offset: int = 0, mask=None, positions=None):
+    """Masks and positions of drafted trees: parents int32 [T] (node numbers within a request), cu_q int32 [B + 1], kv_len int32 [B] with the new
+    tokens.  Returns (mask int32 [T, words], positions int32 [T])."""
+    if mask is not None and positions is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_tree(parents, cu_q, kv_len, words, position_offset, mask, positions)
+        if rc == PQ_OK:
+            return mask, positions
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_tree")
+    T, B = parents.numel(), kv_len.numel()
+    if mask is None:
+        mask = torch.empty((T, int(words)), dtype=torch.int32, device=parents.device)
+    if positions is None:
+        positions = torch.empty((T,), dtype=torch.int32, device=parents.device)
+    for t, what in ((parents, "parents"), (cu_q, "cu_q"), (kv_len, "kv_len"), (mask, "mask"), (positions, "positions")):
+        _here(t, torch.int32, what)
+    if cu_q.numel() != B + 1 or mask.numel() < T * int(words) or positions.numel() < T:
+        raise ValueError("shape mismatch")
+    _check(lib().pq_kv4_tree(_ptr(parents), _ptr(cu_q), _ptr(kv_len), B, T, int(words), int(position_offset), _ptr(mask), _ptr(positions),
+                             _stream()), "pq_kv4_tree")
+    return mask, positions
+
+
+def pq_kv4_tree_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, window: int, sinks: int, k_codes) -> int:
+    """Scratch memory of pq_kv4_tree_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
+    return int(lib().pq_kv4_tree_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), int(window), int(sinks),
+                                                           _kv4_sizes(k_codes)))
+
+
+def pq_kv4_tree_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, mask,
+                          window: int = 0, sinks: int = 0, group: int = 0, prefix_k=None, prefix_v=None, out=None, workspace=None):
+    """pq_kv4_attention, where the last tokens of a request of up to 32 * words rows are the nodes of a tree and a row sees those of its mask
+    (int32 [T, words], pq_kv4_tree's); window 0: all of the history.  Returns (out, workspace)."""
+    if out is not None and workspace is not None:
+        if _lib is None:
+            lib()
+        rc = _call.kv4_tree_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k,
+                                      prefix_v, mask, window, sinks, out, workspace)
+        if rc == PQ_OK:
+            return out, workspace
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_tree_attention")
+    cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
+    _here(mask, torch.int32, "mask")
+    if mask.dim() != 2 or mask.shape[0] != q.shape[0]:
+        raise ValueError("shape mismatch")
+    size = (int(window), int(sinks))
+    return _kv4_attend("pq_kv4_tree_attention", q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v,
+                       (_ptr(mask), mask.shape[1]) + size, size, out, workspace)
+
+
+def pq_kv4_accept(tokens, parents, chosen, cu_q, kv_len, block_table, page_size: int, words: int, depth: int, free_pages=None, taken=None,
+                  accepted=None, next_token=None, path=None, kv_len_out=None, from_slots=None, to_slots=None, taken_out=None):
+    """What stays of drafted trees: tokens, parents, chosen int32 [T], the rest as pq_kv4_slots left it; the pages of what does not stay go back to
+    free_pages (written).  Returns (accepted, next_token int32 [B], path int32 [B, depth], kv_len_out int32 [B], from_slots, to_slots int64
+    [B, depth], taken_out int32 [1])."""
+    outs = (accepted, next_token, path, kv_len_out, from_slots, to_slots, taken_out)
+    if all(t is not None for t in outs):
+        if _lib is None:
+            lib()
+        rc = _call.kv4_accept(tokens, parents, chosen, cu_q, kv_len, block_table, page_size, words, depth, free_pages, taken, *outs)
+        if rc == PQ_OK:
+            return outs
+        if rc > 0:
+            raise PQError(rc, "pq_kv4_accept")
+    T, B, depth = tokens.numel(), kv_len.numel(), int(depth)
+    if depth < 1:
+        raise PQError(PQ_ERR_SHAPE, "pq_kv4_accept")
+    sizes = (("accepted", B), ("next_token", B), ("path", B * depth), ("kv_len_out", B), ("from_slots", B * depth), ("to_slots", B * depth), ("taken_out", 1))
+    made = []
+    for t, (what, n) in zip(outs, sizes):
+        kind = torch.int64 if what.endswith("slots") else torch.int32
+        if t is None:
+            t = torch.empty((B, depth) if n == B * depth and what in ("path", "from_slots", "to_slots") else (n,), dtype=kind, device=kv_len.device)
+        _here(t, kind, what)
+        if t.numel() < n:
+            raise ValueError("shape mismatch")
+        made.append(t)
+    for t, what in ((tokens, "tokens"), (parents, "parents"), (chosen, "chosen"), (cu_q, "cu_q"), (kv_len, "kv_len"), (block_table, "block_table")):
+        _here(t, torch.int32, what)
+    for t, what in ((free_pages, "free_pages"), (taken, "taken")):
+        if t is not None:
+            _here(t, torch.int32, what)
+    if (free_pages is None) != (taken is None):
+        raise ValueError("free_pages and taken come together")
+    if (parents.numel() != T or chosen.numel() != T or cu_q.numel() != B + 1 or block_table.dim() != 2 or block_table.shape[0] != B or
+            (taken is not None and taken.numel() < 1)):
+        raise ValueError("shape mismatch")
+    _check(lib().pq_kv4_accept(_ptr(tokens), _ptr(parents), _ptr(chosen), _ptr(cu_q), _ptr(kv_len), B, T, int(words), depth, _ptr(block_table),
+                               block_table.shape[1], int(page_size), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), _ptr(taken),
+                               *(_ptr(t) for t in made), _stream()), "pq_kv4_accept")
+    return tuple(made)
+
+
+class KV4Layers:
+    """The caches of a model's layers, as pq_kv4_keep takes them: made once, of (k_codes, v_codes, k_scale, v_scale) of every layer.  It holds the
+    tensors."""
+
+    def __init__(self, layers, group: int = 0):
+        self.tensors = tuple(tuple(layer) for layer in layers)
+        self.group = int(group)
+        if not self.tensors:
+            raise ValueError("no layers")
+        first = self.tensors[0][0]
+        if any(layer[0].shape != first.shape or layer[0].device != first.device for layer in self.tensors):
+            raise ValueError("shape mismatch")
+        self.device = first.get_device()
+        self.caches = (KV4Cache * len(self.tensors))(*(_kv4_cache(*layer, self.group) for layer in self.tensors))
+        self.count = len(self.tensors)
+        self.address = ctypes.addressof(self.caches)
+
+
+def pq_kv4_keep(from_slots, to_slots, layers: KV4Layers):
+    """The codes (and dynamic steps) of from_slots int64 [B, width] go to to_slots, in every layer; -1 moves nothing."""
+    if _lib is None:
+        lib()
+    rc = _call.kv4_keep(from_slots, to_slots, layers.address, layers.count, layers.device)
+    if rc == PQ_OK:
+        return
+    if rc > 0:
+        raise PQError(rc, "pq_kv4_keep")
+    _here(from_slots, torch.int64, "from_slots")
+    _here(to_slots, torch.int64, "to_slots")
+    if from_slots.dim() != 2 or to_slots.shape != from_slots.shape:
+        raise ValueError("shape mismatch")
+    if layers.device != torch._C._cuda_getDevice():
+        raise ValueError("layers must lie on the current device")
+    _check(lib().pq_kv4_keep(_ptr(from_slots), _ptr(to_slots), from_slots.shape[0], from_slots.shape[1], layers.caches, layers.count, _stream()),
+           "pq_kv4_keep")
 
 
 def pq_set_gemm_variant(variant: int) -> int:

@@ -1,4 +1,4 @@
-// The call path of the smallest calls, pq_linear and pq_linear2 with the caller's own output and workspace and the three calls of a step on
+// The call path of the smallest calls, pq_linear and pq_linear2 with the caller's own output and workspace and the calls of a step on
 // the paged 4-bit cache with the caller's own outputs, in native code: argument checks, pointers and the current stream.  A decoded token's kernel takes 4.0 us (1 x 4096 -> 4096), the call through
 // Python attributes and ctypes 5.5 us of host time, of which 3.5 are ctypes and the launch; here the whole call takes 3.4 us
 // (1 x 4096 -> 4096, eager, weights in turn: 5.95 -> 4.33 us a call).
@@ -117,9 +117,19 @@ PyObject* linear2(PyObject*, PyObject* const* a, Py_ssize_t n)
 using Slots = decltype(&pq_kv4_slots);
 using Append = decltype(&pq_kv4_append);
 using Attention = decltype(&pq_kv4_attention);
+using WindowAttention = decltype(&pq_kv4_window_attention);
+using Tree = decltype(&pq_kv4_tree);
+using TreeAttention = decltype(&pq_kv4_tree_attention);
+using Accept = decltype(&pq_kv4_accept);
+using Keep = decltype(&pq_kv4_keep);
 Slots g_slots = nullptr;
 Append g_append = nullptr;
 Attention g_attention = nullptr;
+WindowAttention g_window_attention = nullptr;
+Tree g_tree = nullptr;
+TreeAttention g_tree_attention = nullptr;
+Accept g_accept = nullptr;
+Keep g_keep = nullptr;
 
 bool here(const at::Tensor& t) { return t.get_device() == c10::hip::current_device(); }
 bool operand_here(PyObject* o, at::ScalarType type, const at::Tensor** t) { return operand(o, type, t) && here(**t); }
@@ -228,35 +238,173 @@ PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(-1);
 }
 
-// (q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k or None, prefix_v or None, causal,
-//  out, workspace)
+// What the three attentions share: (q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale, max_q, group, prefix_k or None,
+// prefix_v or None) in front, (out, workspace) at the end.
+struct Attended {
+    const at::Tensor *q, *cu, *kv, *table, *pk, *pv, *out, *ws;
+    int64_t max_q, group, heads, B;
+    pq_kv4_cache c;
+    float scale;
+    int32_t n_prefix;
+
+    bool from(PyObject* const* a, PyObject* const* last)
+    {
+        if (!rows_here(a[0], &q) || !operand_here(a[1], at::kInt, &cu) || !operand_here(a[2], at::kInt, &kv) || !operand_here(a[3], at::kInt, &table) ||
+            !PyFloat_CheckExact(a[8]) || !whole(a[9], 1, INT32_MAX, &max_q) || !whole(a[10], 0, INT32_MAX, &group) || !cache_here(a + 4, group, &c) ||
+            !optional_here(a[11], at::kHalf, &pk) || !optional_here(a[12], at::kHalf, &pv) || !operand_here(last[0], at::kHalf, &out) ||
+            !operand_here(last[1], at::kByte, &ws))
+            return false;
+        const int64_t D = c.head_dim;
+        B = kv->numel();
+        heads = D ? q->size(1) / D : 0;
+        const bool prefix = pk && pk->dim() == 3 && pk->size(1) == c.n_kv_heads && pk->size(2) == D && pv && pv->sizes() == pk->sizes();
+        if (heads <= 0 || heads * D != q->size(1) || heads > INT32_MAX || cu->numel() != B + 1 || table->dim() != 2 || table->size(0) != B ||
+            table->size(1) > INT32_MAX || B > INT32_MAX || !(prefix || (!pk && !pv)) || (prefix && pk->size(0) > INT32_MAX) ||
+            out->numel() < q->size(0) * heads * D)
+            return false;
+        n_prefix = prefix ? (int32_t)pk->size(0) : 0;
+        scale = (float)PyFloat_AS_DOUBLE(a[8]);
+        return true;
+    }
+
+    template <typename F, typename... Sight> PyObject* call(F f, Sight... sight) const
+    {
+        void* const st = stream();
+        const int64_t stride = row_stride(*q);
+        void *qp = q->data_ptr(), *op = out->data_ptr(), *wp = ws->data_ptr(), *pkp = pointer(pk), *pvp = pointer(pv);
+        const int32_t *cup = as<int32_t>(cu), *kvp = as<int32_t>(kv), *tp = as<int32_t>(table);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = f(qp, stride, q->size(0), (int32_t)heads, cup, kvp, (int32_t)B, (int32_t)max_q, tp, (int32_t)table->size(1), &c, pkp, pvp,
+               n_prefix, scale, sight..., op, wp, (size_t)ws->numel(), st);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(rc);
+    }
+};
+
+// (..., causal, out, workspace)
 PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     try {
-        const at::Tensor *q, *cu, *kv, *table, *pk, *pv, *out, *ws;
-        int64_t max_q, group;
-        pq_kv4_cache c;
-        if (n == 16 && g_attention && rows_here(a[0], &q) && operand_here(a[1], at::kInt, &cu) && operand_here(a[2], at::kInt, &kv) &&
-            operand_here(a[3], at::kInt, &table) && PyFloat_CheckExact(a[8]) && whole(a[9], 1, INT32_MAX, &max_q) &&
-            whole(a[10], 0, INT32_MAX, &group) && cache_here(a + 4, group, &c) && optional_here(a[11], at::kHalf, &pk) &&
-            optional_here(a[12], at::kHalf, &pv) && PyBool_Check(a[13]) && operand_here(a[14], at::kHalf, &out) &&
-            operand_here(a[15], at::kByte, &ws)) {
-            const int64_t T = q->size(0), D = c.head_dim, B = kv->numel(), heads = D ? q->size(1) / D : 0;
-            const bool prefix = pk && pk->dim() == 3 && pk->size(1) == c.n_kv_heads && pk->size(2) == D && pv && pv->sizes() == pk->sizes();
-            if (heads > 0 && heads * D == q->size(1) && heads <= INT32_MAX && cu->numel() == B + 1 && table->dim() == 2 && table->size(0) == B &&
-                table->size(1) <= INT32_MAX && B <= INT32_MAX && (prefix || (!pk && !pv)) && (!prefix || pk->size(0) <= INT32_MAX) &&
-                out->numel() >= T * heads * D) {
-                const float scale = (float)PyFloat_AS_DOUBLE(a[8]);
-                const int causal = a[13] == Py_True;
+        Attended x;
+        if (n == 16 && g_attention && PyBool_Check(a[13]) && x.from(a, a + 14)) return x.call(g_attention, (int32_t)(a[13] == Py_True));
+    } catch (...) {
+    }
+    return PyLong_FromLong(-1);
+}
+
+// (..., window, sinks, out, workspace)
+PyObject* kv4_window_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    try {
+        Attended x;
+        int64_t window, sinks;
+        if (n == 17 && g_window_attention && whole(a[13], 0, INT32_MAX, &window) && whole(a[14], 0, INT32_MAX, &sinks) && x.from(a, a + 15))
+            return x.call(g_window_attention, (int32_t)window, (int32_t)sinks);
+    } catch (...) {
+    }
+    return PyLong_FromLong(-1);
+}
+
+// (..., mask, window, sinks, out, workspace)
+PyObject* kv4_tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    try {
+        Attended x;
+        const at::Tensor* mask;
+        int64_t window, sinks;
+        if (n == 18 && g_tree_attention && operand_here(a[13], at::kInt, &mask) && whole(a[14], 0, INT32_MAX, &window) &&
+            whole(a[15], 0, INT32_MAX, &sinks) && x.from(a, a + 16) && mask->dim() == 2 && mask->size(0) == x.q->size(0) && mask->size(1) <= INT32_MAX)
+            return x.call(g_tree_attention, (const int32_t*)as<int32_t>(mask), (int32_t)mask->size(1), (int32_t)window, (int32_t)sinks);
+    } catch (...) {
+    }
+    return PyLong_FromLong(-1);
+}
+
+// (parents, cu_q, kv_len, words, position_offset, mask, positions)
+PyObject* kv4_tree(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    try {
+        const at::Tensor *parents, *cu, *kv, *mask, *pos;
+        int64_t words, offset;
+        if (n == 7 && g_tree && operand_here(a[0], at::kInt, &parents) && operand_here(a[1], at::kInt, &cu) && operand_here(a[2], at::kInt, &kv) &&
+            whole(a[3], 0, 256, &words) && whole(a[4], 0, INT32_MAX, &offset) && operand_here(a[5], at::kInt, &mask) &&
+            operand_here(a[6], at::kInt, &pos)) {
+            const int64_t T = parents->numel(), B = kv->numel();
+            if (cu->numel() == B + 1 && B <= INT32_MAX && mask->numel() / (words > 0 ? words : 1) >= T && pos->numel() >= T) {
                 void* const st = stream();
+                const int32_t *pp = as<int32_t>(parents), *cup = as<int32_t>(cu), *kvp = as<int32_t>(kv);
+                int32_t *mp = as<int32_t>(mask), *posp = as<int32_t>(pos);
                 int rc;
                 Py_BEGIN_ALLOW_THREADS
-                rc = g_attention(q->data_ptr(), row_stride(*q), T, (int32_t)heads, as<int32_t>(cu), as<int32_t>(kv), (int32_t)B, (int32_t)max_q,
-                                 as<int32_t>(table), (int32_t)table->size(1), &c, pointer(pk), pointer(pv), prefix ? (int32_t)pk->size(0) : 0, scale,
-                                 causal, out->data_ptr(), ws->data_ptr(), (size_t)ws->numel(), st);
+                rc = g_tree(pp, cup, kvp, (int32_t)B, T, (int32_t)words, (int32_t)offset, mp, posp, st);
                 Py_END_ALLOW_THREADS
                 return PyLong_FromLong(rc);
             }
+        }
+    } catch (...) {
+    }
+    return PyLong_FromLong(-1);
+}
+
+// (tokens, parents, chosen, cu_q, kv_len, block_table, page_size, words, depth, free_pages or None, taken or None, accepted, next_token, path,
+//  kv_len_out, from_slots, to_slots, taken_out)
+PyObject* kv4_accept(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    try {
+        const at::Tensor *tokens, *parents, *chosen, *cu, *kv, *table, *free_pages, *taken, *accepted, *next, *path, *kv_out, *from, *to, *taken_out;
+        int64_t ps, words, depth;
+        if (n == 18 && g_accept && operand_here(a[0], at::kInt, &tokens) && operand_here(a[1], at::kInt, &parents) && operand_here(a[2], at::kInt, &chosen) &&
+            operand_here(a[3], at::kInt, &cu) && operand_here(a[4], at::kInt, &kv) && operand_here(a[5], at::kInt, &table) &&
+            whole(a[6], 0, INT32_MAX, &ps) && whole(a[7], 0, 256, &words) && whole(a[8], 0, INT32_MAX, &depth) &&
+            optional_here(a[9], at::kInt, &free_pages) && optional_here(a[10], at::kInt, &taken) && operand_here(a[11], at::kInt, &accepted) &&
+            operand_here(a[12], at::kInt, &next) && operand_here(a[13], at::kInt, &path) && operand_here(a[14], at::kInt, &kv_out) &&
+            operand_here(a[15], at::kLong, &from) && operand_here(a[16], at::kLong, &to) && operand_here(a[17], at::kInt, &taken_out)) {
+            const int64_t T = tokens->numel(), B = kv->numel(), d = depth > 0 ? depth : 1;
+            if (parents->numel() == T && chosen->numel() == T && cu->numel() == B + 1 && B <= INT32_MAX && table->dim() == 2 && table->size(0) == B &&
+                table->size(1) <= INT32_MAX && !free_pages == !taken && (!taken || taken->numel() >= 1) &&
+                (!free_pages || free_pages->numel() <= INT32_MAX) && accepted->numel() >= B && next->numel() >= B && path->numel() / d >= B &&
+                kv_out->numel() >= B && from->numel() / d >= B && to->numel() / d >= B && taken_out->numel() >= 1) {
+                void* const st = stream();
+                int32_t* p[13];                    // (in front of the call: without the lock nothing may be thrown)
+                int k = 0;
+                for (const at::Tensor* t : {tokens, parents, chosen, cu, kv, table, free_pages, taken, accepted, next, path, kv_out, taken_out}) p[k++] = as<int32_t>(t);
+                int64_t *fp = as<int64_t>(from), *tp = as<int64_t>(to);
+                const int32_t W = (int32_t)table->size(1), n_free = free_pages ? (int32_t)free_pages->numel() : 0;
+                int rc;
+                Py_BEGIN_ALLOW_THREADS
+                rc = g_accept(p[0], p[1], p[2], p[3], p[4], (int32_t)B, T, (int32_t)words, (int32_t)depth, p[5], W, (int32_t)ps, p[6], n_free, p[7], p[8],
+                              p[9], p[10], p[11], fp, tp, p[12], st);
+                Py_END_ALLOW_THREADS
+                return PyLong_FromLong(rc);
+            }
+        }
+    } catch (...) {
+    }
+    return PyLong_FromLong(-1);
+}
+
+// (from_slots, to_slots, address of the caches, their number, their device)
+PyObject* kv4_keep(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    try {
+        const at::Tensor *from, *to;
+        int64_t count, device;
+        if (n == 5 && g_keep && operand_here(a[0], at::kLong, &from) && operand_here(a[1], at::kLong, &to) && PyLong_CheckExact(a[2]) &&
+            whole(a[3], 1, INT32_MAX, &count) && whole(a[4], 0, INT32_MAX, &device) && device == c10::hip::current_device() && from->dim() == 2 &&
+            to->sizes() == from->sizes() && from->size(0) <= INT32_MAX && from->size(1) <= INT32_MAX) {
+            const auto* caches = static_cast<const pq_kv4_cache*>(PyLong_AsVoidPtr(a[2]));
+            if (!caches) {
+                PyErr_Clear();
+                return PyLong_FromLong(-1);
+            }
+            void* const st = stream();
+            const int64_t *fp = as<int64_t>(from), *tp = as<int64_t>(to);
+            int rc;
+            Py_BEGIN_ALLOW_THREADS
+            rc = g_keep(fp, tp, (int32_t)from->size(0), (int32_t)from->size(1), caches, (int32_t)count, st);
+            Py_END_ALLOW_THREADS
+            return PyLong_FromLong(rc);
         }
     } catch (...) {
     }
@@ -271,6 +419,19 @@ PyObject* bind_kv4(PyObject*, PyObject* args)
     g_slots = reinterpret_cast<Slots>(static_cast<uintptr_t>(s));
     g_append = reinterpret_cast<Append>(static_cast<uintptr_t>(ap));
     g_attention = reinterpret_cast<Attention>(static_cast<uintptr_t>(at));
+    Py_RETURN_NONE;
+}
+
+// (addresses of pq_kv4_window_attention, pq_kv4_tree, pq_kv4_tree_attention, pq_kv4_accept and pq_kv4_keep)
+PyObject* bind_kv4_more(PyObject*, PyObject* args)
+{
+    unsigned long long w, t, ta, ac, k;
+    if (!PyArg_ParseTuple(args, "KKKKK", &w, &t, &ta, &ac, &k)) return nullptr;
+    g_window_attention = reinterpret_cast<WindowAttention>(static_cast<uintptr_t>(w));
+    g_tree = reinterpret_cast<Tree>(static_cast<uintptr_t>(t));
+    g_tree_attention = reinterpret_cast<TreeAttention>(static_cast<uintptr_t>(ta));
+    g_accept = reinterpret_cast<Accept>(static_cast<uintptr_t>(ac));
+    g_keep = reinterpret_cast<Keep>(static_cast<uintptr_t>(k));
     Py_RETURN_NONE;
 }
 
@@ -291,6 +452,12 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"kv4_slots", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_slots)), METH_FASTCALL, nullptr},
                          {"kv4_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_append)), METH_FASTCALL, nullptr},
                          {"kv4_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_attention)), METH_FASTCALL, nullptr},
+                         {"bind_kv4_more", bind_kv4_more, METH_VARARGS, nullptr},
+                         {"kv4_window_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_window_attention)), METH_FASTCALL, nullptr},
+                         {"kv4_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_tree)), METH_FASTCALL, nullptr},
+                         {"kv4_tree_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_tree_attention)), METH_FASTCALL, nullptr},
+                         {"kv4_accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_accept)), METH_FASTCALL, nullptr},
+                         {"kv4_keep", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_keep)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pq_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

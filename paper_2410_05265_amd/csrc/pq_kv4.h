@@ -56,15 +56,60 @@ struct AttentionArgs {
     float softmax_scale;
     int32_t causal;
     __half* out;
+    // What rows see of a history (Masked kernels): its first `sinks` tokens and the last `window` before the row's own end, and of a tree's
+    // nodes those of its mask, uint32 [T, words] (null: no trees).
+    const uint32_t* tree;
+    int32_t words;
+    int32_t window;         // 1 .. kWidestWindow
+    int32_t sinks;
 };
+constexpr int32_t kWidestWindow = (1 << 30) - 1;       // (no table holds as many tokens)
+
+constexpr int kMostNodes = 256;         // of a tree: eight words of mask
 
 int launch_slots(const int32_t* kv_len, const int32_t* q_len, int32_t B, int32_t* block_table, int32_t table_pages,
                  const int32_t* free_pages, int32_t n_free, const int32_t* taken, int32_t log2_page, int32_t T, int32_t position_offset,
                  int32_t* cu_q, int32_t* kv_len_out, int32_t* positions, int64_t* slots, int32_t* taken_out, hipStream_t st);
 int launch_append(const AppendArgs& a, int32_t head_dim, int32_t group, bool rotate, hipStream_t st);
 
+struct AcceptArgs {
+    const int32_t* tokens;
+    const int32_t* parents;
+    const int32_t* chosen;
+    const int32_t* cu_q;
+    const int32_t* kv_len;
+    int32_t B;
+    int32_t T;
+    int32_t words;
+    int32_t depth;
+    const int32_t* table;
+    int32_t table_pages;
+    int32_t log2_page;
+    int32_t* free_pages;
+    int32_t n_free;
+    const int32_t* taken;
+    int32_t* accepted;
+    int32_t* next_token;
+    int32_t* path;
+    int32_t* kv_len_out;
+    int64_t* from_slots;
+    int64_t* to_slots;
+    int32_t* taken_out;
+};
+
+int launch_tree(const int32_t* parents, const int32_t* cu_q, const int32_t* kv_len, int32_t B, int32_t T, int32_t words, int32_t position_offset,
+                uint32_t* mask, int32_t* positions, hipStream_t st);
+int launch_accept(const AcceptArgs& a, hipStream_t st);
+int launch_keep(const int64_t* from_slots, const int64_t* to_slots, int32_t B, int32_t width, const pq_kv4_cache* caches, int32_t n_caches, hipStream_t st);
+
+// capacity: tokens of a history, at most; with a window what one row and those beside it see.
+inline int64_t seen_at_most(int64_t capacity, int32_t max_q, int32_t window, int32_t sinks)
+{
+    const int64_t most = (int64_t)window + sinks + max_q + 128;
+    return most < capacity ? most : capacity;
+}
 size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity);
-int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, void* ws, hipStream_t st);
+int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, bool masked, void* ws, hipStream_t st);
 
 }  // namespace kv4
 }  // namespace pq

@@ -123,9 +123,75 @@ __device__ __forceinline__ int sees(const AttentionArgs& a, const Request& r, in
     return a.causal ? min(max(r.sees + token, 0), r.n) : r.n;
 }
 
+// ---- Windows, and trees of drafted tokens: the kernels' variants with `Masked` among their parameters.
+//
+// A request of at most 32 * words rows is a tree, of which c = sees - 1 tokens lie in front: row i sees t < c with t < sinks or t >= c + |mask_i| - window,
+// and node j, the token c + j, if its mask says so.  Any other is a chain: row i sees t < sees + i with t < sinks or t >= sees + i - window.
+struct Masked;
+
+__device__ __forceinline__ bool is_tree(const AttentionArgs& a, const Request& r) { return a.tree != nullptr && r.q_len <= 32 * a.words; }
+
+// Tokens that a row sees: t < limit with t < sinks or t >= lo; of a tree's the nodes behind are in its mask.
+struct Row { int limit, lo; };
+
+// Word w of the mask of a row: nodes that there are.
+__device__ __forceinline__ uint32_t mask_word(const AttentionArgs& a, const Request& r, int token, int w)
+{
+    if (w < 0 || w >= a.words) return 0;
+    const int nodes = r.q_len - 32 * w;
+    const uint32_t there = nodes >= 32 ? ~0u : nodes > 0 ? (1u << nodes) - 1 : 0u;
+    return a.tree[(int64_t)(r.start + token) * a.words + w] & there;
+}
+
+// Nodes first .. first + 31 (first may be negative) in a row's mask.
+__device__ __forceinline__ uint32_t mask_bits(const AttentionArgs& a, const Request& r, int token, int first)
+{
+    const int w = first >> 5;
+    return __builtin_amdgcn_alignbit(mask_word(a, r, token, w + 1), mask_word(a, r, token, w), first & 31);
+}
+
+__device__ __forceinline__ Row masked_row(const AttentionArgs& a, const Request& r, int token)
+{
+    if (!is_tree(a, r)) return {min(max(r.sees + token, 0), r.n), max(r.sees + token - a.window, 0)};
+    const int c = r.sees - 1;
+    int nodes = 0;
+    if (a.window < kWidestWindow) {
+        for (int w = 0; w < a.words; ++w) nodes += __builtin_popcount(mask_word(a, r, token, w));
+    }
+    return {min(max(c, 0), r.n), max(c - a.window + nodes, 0)};
+}
+
+// What the rows of tokens first .. last of a request see, as far as no mask has to be read.
+struct Seen {
+    int all;       // every row sees the tokens before it, but for the window
+    int any;       // no row sees one from it on
+    int lo, lo_top;    // tokens before lo that are no sinks are seen by no row, those from lo_top on are hidden by no row's window
+};
+__device__ __forceinline__ Seen masked_rows(const AttentionArgs& a, const Request& r, int first, int last)
+{
+    if (is_tree(a, r)) {
+        const int c = r.sees - 1;
+        return {min(max(c, 0), r.n), min(max(c + r.q_len, 0), r.n), min(max(c - a.window, 0), r.n), max(c - a.window + r.q_len, 0)};
+    }
+    return {min(max(r.sees + first, 0), r.n), min(max(r.sees + last, 0), r.n), min(max(r.sees + first - a.window, 0), r.n),
+            max(r.sees + last - a.window, 0)};
+}
+
+// A history in tiles of SIZE tokens, without those that only hold tokens between the sinks and the window: tile number i of what is left.
+template <int SIZE> struct Tiles {
+    int front, gap;                                // tiles of the sinks, and those left out behind them
+    __device__ __forceinline__ Tiles(const AttentionArgs& a, int lo) : front((int)(((int64_t)a.sinks + SIZE - 1) / SIZE)), gap(max(lo / SIZE - front, 0)) {}
+    __device__ __forceinline__ int at(int i) const { return i + (i >= front ? gap : 0); }
+    __device__ __forceinline__ int count(int end) const         // of the tokens before `end`
+    {
+        const int all = (end + SIZE - 1) / SIZE;
+        return all <= front ? all : max(all - gap, front);
+    }
+};
+
 // Requests of more than small_rows rows (tokens times query heads of a key/value head); the others are the row kernel's.
 size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity);
-int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st);
+int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, int64_t capacity, bool masked, float* partial, hipStream_t st);
 
 }  // namespace kv4
 }  // namespace pq

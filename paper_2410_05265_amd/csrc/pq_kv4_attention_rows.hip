@@ -32,7 +32,16 @@ constexpr int kDepth = 4;                          // places of a wavefront's ri
 constexpr int kPerCu = 2, kGroups = 256 * kPerCu;
 constexpr float kLeast = 0x1.0p-80f;               // smallest reference of value weights (dynamic steps)
 
-__device__ __forceinline__ int64_t units_of_tile(const Request& r) { return r.n > 0 ? (r.n + kTile - 1) / kTile : 1; }
+// Units of every tile of a request's rows: those of all its tokens, with MASKED of those that one of its rows may see.
+template <bool MASKED>
+__device__ __forceinline__ int64_t units_of_tile(const AttentionArgs& a, const Request& r)
+{
+    if constexpr (MASKED) {
+        const Seen s = masked_rows(a, r, 0, max(r.q_len - 1, 0));
+        return max(Tiles<kTile>(a, s.lo).count(s.any), 1);
+    }
+    return r.n > 0 ? (r.n + kTile - 1) / kTile : 1;
+}
 
 // Histories of a request: heads x tiles of rows; none if it has more than small_rows rows.
 template <int ROWS>
@@ -56,7 +65,7 @@ struct Plan {
     Request r;                           // the last of them
 };
 
-template <int ROWS>
+template <int ROWS, bool MASKED>
 __device__ __forceinline__ Plan plan(const AttentionArgs& a, int small_rows, int lane)
 {
     Plan p;
@@ -70,7 +79,7 @@ __device__ __forceinline__ Plan plan(const AttentionArgs& a, int small_rows, int
         p.r = request(a, b);
         const int64_t n = (int64_t)tiles_of<ROWS>(a, p.r, small_rows) * a.cache.n_kv_heads;
         items += n;
-        p.own += n * units_of_tile(p.r);
+        p.own += n * units_of_tile<MASKED>(a, p.r);
     }
     int64_t units_incl = p.own, items_incl = items;
 #pragma unroll
@@ -132,9 +141,10 @@ struct Shape {
     static constexpr size_t kLds = (size_t)kWaves * kDepth * SLOT;
 };
 
-template <int D, int G, bool DYNAMIC, int CB>
+template <int D, int G, bool DYNAMIC, int CB, typename... KIND>
 __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(AttentionArgs a, float* partial, Item* items, int64_t most_items, int small_rows)
 {
+    constexpr bool MASKED = sizeof...(KIND) > 0;
     typedef Shape<D, G, DYNAMIC, CB> S;
     constexpr int NG = S::NG, KS = S::KS, CH = S::CH, ROWS = S::ROWS;
     extern __shared__ __align__(256) uint8_t lds[];
@@ -144,7 +154,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
     const uint8_t* const ring = lds + wave * kDepth * S::SLOT;
     const uint32_t ring_addr = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)ring;
 
-    const Plan p = plan<ROWS>(a, small_rows, lane);
+    const Plan p = plan<ROWS, MASKED>(a, small_rows, lane);
     // Codes that one wavefront reads once go past the caches, where they would push out each other and, from call to call, themselves: a call's
     // history from 64 MiB on (356 MB 82 -> 73.5 us, 148 MB 43.2 -> 39.8, 342 MB with dynamic steps 84.5 -> 79.9); below, they may be in the
     // memory-side cache still, where a program has few caches: three in turn, through the caches | past them, 32 MB 18.5 | 19.1, 59 MB 26.5 |
@@ -175,8 +185,9 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             for (; at < p.last; ++at) {
                 r = request(a, at);
                 const int64_t n = (int64_t)tiles_of<ROWS>(a, r, small_rows) * Hkv;
-                if (range < u + n * units_of_tile(r)) break;
-                u += n * units_of_tile(r);
+                const int64_t units = n * units_of_tile<MASKED>(a, r);
+                if (range < u + units) break;
+                u += units;
                 i += n;
             }
         }
@@ -192,7 +203,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 
     for (int64_t u0 = range; u0 < range_end;) {
         const int tiles = tiles_of<ROWS>(a, r, small_rows);
-        const int64_t per = units_of_tile(r), whole = per * tiles * Hkv;
+        const int64_t per = units_of_tile<MASKED>(a, r), whole = per * tiles * Hkv;
         if (u0 >= base + whole) {                  // (requests without queries, or with many, have no units)
             base += whole;
             item_base += (int64_t)tiles * Hkv;
@@ -203,8 +214,18 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         const int head = __builtin_amdgcn_readfirstlane((int)item / tiles), tile = __builtin_amdgcn_readfirstlane((int)item % tiles);
         const int rows = r.q_len * per_kv;
         const int first_token = tile * ROWS / per_kv, last_token = min((tile * ROWS + ROWS - 1) / per_kv, r.q_len - 1);
-        const int all_see = sees(a, r, first_token), any_sees = sees(a, r, last_token); // tokens before all_see need no mask
+        const bool tree = MASKED && is_tree(a, r);
+        Seen seen;                                 // (lo: of the request, lo_top: of this tile's rows)
+        if constexpr (MASKED) {
+            seen = masked_rows(a, r, first_token, last_token);
+            seen.lo = masked_rows(a, r, 0, 0).lo;
+        } else {
+            seen = {sees(a, r, first_token), sees(a, r, last_token), 0, 0};
+        }
+        const int all_see = seen.all, any_sees = seen.any;     // tokens before all_see need no mask, but for a window's
+        const Tiles<kTile> left_in(a, MASKED ? seen.lo : 0);
         const int from = (int)(from_unit * kTile), to = (int)min((from_unit + take) * kTile, (int64_t)any_sees);
+        auto start_of = [&](int i) PQ_INLINE -> int { return MASKED ? left_in.at((int)from_unit + i) * kTile : from + i * kTile; };
         if (from_unit == 0 && lane == 0 && item_base + item < most_items)
             items[1 + item_base + item] = {worker, take == per ? 1 : (int)worker_of(u0 + per - 1) - worker + 1, u0 == range ? 0 : 1, r.start, rows, head,
                                            tile * ROWS, 0};
@@ -212,10 +233,11 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         // ---- codes on their way
         const int32_t* table = a.table + (int64_t)b * a.table_pages;
         int ids_from = -64, ids = 0;
-        const int count = __builtin_amdgcn_readfirstlane(from < to ? (to - from + kTile - 1) / kTile : 0);
+        const int count = __builtin_amdgcn_readfirstlane(MASKED ? max((int)min(from_unit + take, (int64_t)left_in.count(any_sees)) - (int)from_unit, 0)
+                                                                : from < to ? (to - from + kTile - 1) / kTile : 0);
         uint32_t bad_bits = 0;                     // two bits for each place of the ring: blocks of 16 tokens whose page is none
         auto fetch = [&](int i) PQ_INLINE {
-            const int t0 = from + i * kTile, place = i % kDepth;
+            const int t0 = start_of(i), place = i % kDepth;
             int64_t first[2];                      // of the blocks, in this head's part of the cache
             bad_bits &= ~(3u << (2 * place));
 #pragma unroll
@@ -257,11 +279,18 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
         };
         // ---- queries: channels as the keys' operands have them
         v4u raw[CB][NG * KS];
-        int limit[CB];                             // tokens that the lane's query sees
+        int limit[CB], lo[CB];                     // tokens that the lane's query sees: before limit, those of no sink from lo on
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             const int row = min(tile * ROWS + 16 * c + col, rows - 1), token = row / per_kv, q_head = head * per_kv + row % per_kv;
-            limit[c] = sees(a, r, token);
+            if constexpr (MASKED) {
+                const Row see = masked_row(a, r, token);
+                limit[c] = see.limit;
+                lo[c] = see.lo;
+            } else {
+                limit[c] = sees(a, r, token);
+                lo[c] = 0;
+            }
             const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
             for (int i = 0; i < NG * KS; ++i) raw[c][i] = *reinterpret_cast<const v4u*>(src + i / KS * G + quarter * (G / 4) + 8 * (i % KS));
@@ -417,7 +446,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 
         // ---- the history
         for (int i = 0; i < count; ++i) {
-            const int t0 = from + i * kTile, place = i % kDepth;
+            const int t0 = start_of(i), place = i % kDepth;
             // until this tile is there; those behind it may be on their way
             const int behind = min(count - 1 - i, kDepth - 1);
             if (behind == 3) wait_vm<3 * S::LOADS>();
@@ -427,7 +456,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
             const uint8_t* const kc = ring + place * S::SLOT;
             const uint8_t* const vc = kc + S::CODES;
             const bool bad0 = (bad_bits >> (2 * place)) & 1, bad1 = (bad_bits >> (2 * place + 1)) & 1;
-            const bool masked = t0 + kTile > all_see || bad0 || bad1;
+            const bool masked = t0 + kTile > all_see || bad0 || bad1 || (MASKED && t0 < seen.lo_top && t0 + kTile > a.sinks);
             uint32_t k[2][NG * KS], v[8][NG];
             v4f ks[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1], vs[DYNAMIC ? 2 : 1][DYNAMIC ? NG : 1];
             // (steps of four tokens, NG each, one after another; every 32 steps of keys are followed by 32 of values)
@@ -501,6 +530,19 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 #pragma unroll
                 for (int c = 0; c < CB; ++c) {
                     const int left = limit[c] - (t0 + 4 * quarter);
+                    if constexpr (MASKED) {
+                        uint32_t nodes = 0;        // of the tree, tokens that the query sees behind its limit
+                        if (tree && t0 + kTile > all_see)
+                            nodes = mask_bits(a, r, min(tile * ROWS + 16 * c + col, rows - 1) / per_kv, t0 - (r.sees - 1)) >> (4 * quarter);
+                        const int hidden = lo[c] - (t0 + 4 * quarter), front = a.sinks - (t0 + 4 * quarter);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int at = 16 * (j >> 2) + (j & 3);
+                            const bool sees_it = at < left ? at >= hidden || at < front : (nodes >> at) & 1;
+                            if (!sees_it || (j < 4 ? bad0 : bad1)) x[c][j] = -INFINITY;
+                        }
+                        continue;
+                    }
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (16 * (j >> 2) + (j & 3) >= left || (j < 4 ? bad0 : bad1)) x[c][j] = -INFINITY;
@@ -766,14 +808,14 @@ size_t partial_bytes(int64_t groups, int32_t head_dim, int blocks)
     return (size_t)(groups < kGroups ? groups : kGroups) * kWaves * 2 * 16 * blocks * (head_dim + 4) * sizeof(float);
 }
 
-template <int D, int G, bool DYNAMIC, int CB>
-int launch(const AttentionArgs& a, int small_rows, void* ws, hipStream_t st)
+template <int D, int G, bool DYNAMIC, int CB, typename... KIND>
+int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, hipStream_t st)
 {
     static std::atomic<uint64_t> allowed{0};
     constexpr size_t lds = Shape<D, G, DYNAMIC, CB>::kLds;
-    const auto kernel = k_kv4_attention_rows<D, G, DYNAMIC, CB>;
+    const auto kernel = k_kv4_attention_rows<D, G, DYNAMIC, CB, KIND...>;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, allowed); rc != PQ_OK) return rc;
-    const Most most = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page, small_rows);
+    const Most most = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, capacity, small_rows);
     const int64_t groups = most.groups < kGroups ? most.groups : kGroups;
     float* const partial = static_cast<float*>(ws);
     Item* const items = reinterpret_cast<Item*>(static_cast<uint8_t*>(ws) + partial_bytes(most.groups, D, CB));
@@ -803,18 +845,18 @@ size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_
     return (partial_bytes(most.groups, head_dim, blocks_for(max_q, n_heads / n_kv_heads, most.units)) + (size_t)(most.items + 1) * sizeof(Item) + 255) & ~(size_t)255;
 }
 
-template <int CB>
-int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, void* ws, hipStream_t st)
+template <int CB, typename... KIND>
+int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, int64_t capacity, void* ws, hipStream_t st)
 {
     if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false, CB>(a, small_rows, ws, st);
-        if (group == 32) return launch<64, 32, true, CB>(a, small_rows, ws, st);
-        return launch<64, 64, true, CB>(a, small_rows, ws, st);
+        if (group == 0) return launch<64, 64, false, CB, KIND...>(a, small_rows, capacity, ws, st);
+        if (group == 32) return launch<64, 32, true, CB, KIND...>(a, small_rows, capacity, ws, st);
+        return launch<64, 64, true, CB, KIND...>(a, small_rows, capacity, ws, st);
     }
-    if (group == 0) return launch<128, 128, false, CB>(a, small_rows, ws, st);
-    if (group == 32) return launch<128, 32, true, 1>(a, small_rows, ws, st);
-    if (group == 64) return launch<128, 64, true, CB>(a, small_rows, ws, st);
-    return launch<128, 128, true, CB>(a, small_rows, ws, st);
+    if (group == 0) return launch<128, 128, false, CB, KIND...>(a, small_rows, capacity, ws, st);
+    if (group == 32) return launch<128, 32, true, 1, KIND...>(a, small_rows, capacity, ws, st);
+    if (group == 64) return launch<128, 64, true, CB, KIND...>(a, small_rows, capacity, ws, st);
+    return launch<128, 128, true, CB, KIND...>(a, small_rows, capacity, ws, st);
 }
 
 }  // namespace
@@ -826,17 +868,19 @@ size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t 
     return all > 256 ? all : 256;                  // (0 says that the sizes are refused)
 }
 
-int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, void* ws, hipStream_t st)
+int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, bool masked, void* ws, hipStream_t st)
 {
+    const int64_t table = (int64_t)a.table_pages << a.cache.log2_page, capacity = masked ? seen_at_most(table, max_q, a.window, a.sinks) : table;
     const int small_rows = small_rows_for(max_q, a.heads_per_kv, a.B);
     if (takes_tiles(max_q, a.heads_per_kv)) {
-        const size_t rows = rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, (int64_t)a.table_pages << a.cache.log2_page);
+        const size_t rows = rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, capacity);
         float* const partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + rows);
-        if (const int rc = launch_attention_tiles(a, head_dim, group, small_rows, partial, st); rc != PQ_OK || small_rows == 0) return rc;
+        if (const int rc = launch_attention_tiles(a, head_dim, group, small_rows, capacity, masked, partial, st); rc != PQ_OK || small_rows == 0) return rc;
     }
-    const int64_t units = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page, small_rows).units;
-    return blocks_for(max_q, a.heads_per_kv, units) == 1 ? launch_rows<1>(a, head_dim, group, small_rows, ws, st)
-                                                         : launch_rows<2>(a, head_dim, group, small_rows, ws, st);
+    const int64_t units = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, capacity, small_rows).units;
+    const bool one = blocks_for(max_q, a.heads_per_kv, units) == 1;
+    if (masked) return one ? launch_rows<1, Masked>(a, head_dim, group, small_rows, capacity, ws, st) : launch_rows<2, Masked>(a, head_dim, group, small_rows, capacity, ws, st);
+    return one ? launch_rows<1>(a, head_dim, group, small_rows, capacity, ws, st) : launch_rows<2>(a, head_dim, group, small_rows, capacity, ws, st);
 }
 
 }  // namespace kv4

@@ -156,9 +156,10 @@ struct Lds {
 // Two workgroups to a CU where 128 registers do: one's start and end, and its waits at the barriers, beside the other's products (64 channels,
 // static steps, 32 heads on 8, one | two: 4 prompts of up to 4096 tokens 232 | 206 us, 4 of 4096 390 | 357, 300 queries each over up to 4000 64 |
 // 65, 500 over 33000 178 | 184; with dynamic steps what does not fit is spilled: to 64 channels 347 | 422, 500 over 33000 277 | 531).
-template <int D, int G, bool DYNAMIC>
+template <int D, int G, bool DYNAMIC, typename... KIND>
 __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs a, float* partial, const int32_t* __restrict__ starts, int splits, int small_rows)
 {
+    constexpr bool MASKED = sizeof...(KIND) > 0;
     constexpr int NG = D / G, KS = D / 16, KSG = G / 16, DB = D / 32, DBG = G / 32;
     extern __shared__ __align__(256) uint8_t raw_lds[];
     typedef Lds<D, G, DYNAMIC> L;
@@ -173,19 +174,39 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     const Request r = at.r;
     const int rows = r.q_len * per_kv, row0 = at.tile * kRows;
     const int last_token = min((row0 + kRows - 1) / per_kv, r.q_len - 1);
-    const int visible = __builtin_amdgcn_readfirstlane(sees(a, r, last_token));        // (a division leaves it in a vector register)
-    const int all_tiles = (visible + kTile - 1) / kTile;
+    const bool tree = MASKED && is_tree(a, r);
+    int lo = 0;                                    // no row sees a token before it that is no sink
+    int visible = __builtin_amdgcn_readfirstlane(sees(a, r, last_token));              // (a division leaves it in a vector register)
+    if constexpr (MASKED) {
+        const Seen seen = masked_rows(a, r, row0 / per_kv, last_token);
+        visible = __builtin_amdgcn_readfirstlane(seen.any);
+        lo = __builtin_amdgcn_readfirstlane(seen.lo);
+    }
+    const Tiles<kTile> left_in(a, lo);
+    auto tile_at = [&](int i) PQ_INLINE -> int { return MASKED ? left_in.at(i) : i; };
+    const int all_tiles = MASKED ? left_in.count(visible) : (visible + kTile - 1) / kTile;
     const int begin = (int)((int64_t)all_tiles * split / splits), end = (int)((int64_t)all_tiles * (split + 1) / splits);
 
     // this lane's query
     int limit, wave_sees;                    // tokens that it sees, and that all of the wavefront's see
+    int hidden = 0, wave_hidden = 0, row_token;    // a window: those before it that are no sinks it does not see, and some of the wavefront's do not
     v8h q[KS];
     float c0 = 0.0f;                         // -8 sum(q): the codes' offset (dynamic steps: the operands are without it)
     {
         const int row = min(row0 + wave * kCols + col, rows - 1);
         const int token = row / per_kv, q_head = head * per_kv + row % per_kv;
-        limit = sees(a, r, token);
-        wave_sees = __builtin_amdgcn_readfirstlane(sees(a, r, min(row0 + wave * kCols, rows - 1) / per_kv));
+        row_token = token;
+        if constexpr (MASKED) {
+            const Row see = masked_row(a, r, token);
+            const Seen wave_rows = masked_rows(a, r, min(row0 + wave * kCols, rows - 1) / per_kv, min(row0 + wave * kCols + kCols - 1, rows - 1) / per_kv);
+            limit = see.limit;
+            hidden = see.lo;
+            wave_sees = __builtin_amdgcn_readfirstlane(wave_rows.all);
+            wave_hidden = __builtin_amdgcn_readfirstlane(wave_rows.lo_top);
+        } else {
+            limit = sees(a, r, token);
+            wave_sees = __builtin_amdgcn_readfirstlane(sees(a, r, min(row0 + wave * kCols, rows - 1) / per_kv));
+        }
         const __half* src = a.q + (int64_t)(r.start + token) * a.row_stride + (int64_t)q_head * D;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h*>(src + 16 * s + 8 * half);
@@ -262,8 +283,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     Codes next;
     int page = 0;
     if (begin < end) {                             // (on their way while the queries are and the prefix tokens are taken)
-        load(begin, page_of(begin), next);
-        page = page_of(begin + 1);
+        load(tile_at(begin), page_of(tile_at(begin)), next);
+        page = page_of(tile_at(begin + 1));
     }
 
     // ---- prefix tokens, in tiles of 32: a thread's token and eight channels of it
@@ -453,26 +474,41 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
 
     if (begin < end) {
         const float bias = c0 * c1;
-        expand(begin, 0, next);
-        load(begin + 1, page, next);
-        page = page_of(begin + 2);
+        expand(tile_at(begin), 0, next);
+        load(tile_at(begin + 1), page, next);
+        page = page_of(tile_at(begin + 2));
         for (int i = begin; i < end; ++i) {
             const int buf = (i - begin) & 1;
             __syncthreads();                       // tile i is in LDS; nobody reads tile i - 1 any more
-            const int page_after = page_of(i + 3);
+            const int page_after = page_of(tile_at(i + 3)), t0 = tile_at(i) * kTile;
             float x[32];
             v4u p[4];
             scores(buf, x);
-            expand(i + 1, buf ^ 1, next);
-            load(i + 2, page, next);
+            expand(tile_at(i + 1), buf ^ 1, next);
+            load(tile_at(i + 2), page, next);
             page = page_after;
             // what rows do not see, or has no page
-            if (i * kTile + kTile > wave_sees ||
+            if (t0 + kTile > wave_sees || (MASKED && t0 < wave_hidden && t0 + kTile > a.sinks) ||
                 __builtin_amdgcn_readfirstlane(sh.bad[buf][0] | sh.bad[buf][1] | sh.bad[buf][2] | sh.bad[buf][3]) != 0) {
-                const int left = limit - (i * kTile + 4 * half);
+                const int left = limit - (t0 + 4 * half);
+                if constexpr (MASKED) {
+                    uint32_t nodes[2] = {0, 0};    // of the tree, tokens that the query sees behind its limit
+                    if (tree && t0 + kTile > wave_sees) {
+                        nodes[0] = mask_bits(a, r, row_token, t0 - (r.sees - 1)) >> (4 * half);
+                        nodes[1] = mask_bits(a, r, row_token, t0 + 32 - (r.sees - 1)) >> (4 * half);
+                    }
+                    const int from = hidden - (t0 + 4 * half), front = a.sinks - (t0 + 4 * half);
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (8 * (j >> 2) + (j & 3) >= left || sh.bad[buf][j >> 3]) x[j] = -INFINITY;
+                    for (int j = 0; j < 32; ++j) {
+                        const int at = 8 * (j >> 2) + (j & 3);
+                        const bool sees_it = at < left ? at >= from || at < front : (nodes[at >> 5] >> (at & 31)) & 1;
+                        if (!sees_it || sh.bad[buf][j >> 3]) x[j] = -INFINITY;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (8 * (j >> 2) + (j & 3) >= left || sh.bad[buf][j >> 3]) x[j] = -INFINITY;
+                }
             }
             probabilities(x, c1, bias, p);
             if constexpr (DYNAMIC) {
@@ -621,12 +657,12 @@ int splits_for(int64_t tiles, int32_t B, int32_t n_kv_heads, int64_t capacity)
     return best;
 }
 
-template <int D, int G, bool DYNAMIC>
+template <int D, int G, bool DYNAMIC, typename... KIND>
 int launch(const AttentionArgs& a, int64_t tiles, int splits, int small_rows, float* partial, const int32_t* starts, hipStream_t st)
 {
     static std::atomic<uint64_t> allowed{0};
     const size_t out = (size_t)kWaves * kCols * (D + 8) * 2, lds = sizeof(Lds<D, G, DYNAMIC>) > out ? sizeof(Lds<D, G, DYNAMIC>) : out;
-    const auto kernel = k_kv4_attention_tiles<D, G, DYNAMIC>;
+    const auto kernel = k_kv4_attention_tiles<D, G, DYNAMIC, KIND...>;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, allowed); rc != PQ_OK) return rc;
     const int Hkv = a.cache.n_kv_heads;
     kernel<<<(unsigned)(tiles * Hkv * splits), kThreads, lds, st>>>(a, partial, starts, splits, small_rows);
@@ -640,6 +676,20 @@ size_t tiles_partial_bytes(int64_t tiles, int splits, int32_t n_kv_heads, int32_
     return splits > 1 ? (size_t)(tiles * n_kv_heads * splits) * kRows * (head_dim + 2) * sizeof(float) : 0;
 }
 
+template <typename... KIND>
+int launch_shape(const AttentionArgs& a, int32_t head_dim, int32_t group, int64_t tiles, int splits, int small_rows, float* partial, const int32_t* starts, hipStream_t st)
+{
+    if (head_dim == 64) {
+        if (group == 0) return launch<64, 64, false, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+        if (group == 32) return launch<64, 32, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+        return launch<64, 64, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+    }
+    if (group == 0) return launch<128, 128, false, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+    if (group == 32) return launch<128, 32, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+    if (group == 64) return launch<128, 64, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+    return launch<128, 128, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+}
+
 }  // namespace
 
 size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity)
@@ -649,24 +699,17 @@ size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv
     return tiles_partial_bytes(tiles, splits, n_kv_heads, head_dim) + (B > kManyRequests ? ((size_t)(B + 1) * sizeof(int32_t) + 255) & ~(size_t)255 : 0);
 }
 
-int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st)
+int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, int64_t capacity, bool masked, float* partial, hipStream_t st)
 {
     const int64_t tiles = tiles_at_most(a.T, a.B, a.heads_per_kv);
-    const int splits = splits_for(tiles, a.B, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
+    const int splits = splits_for(tiles, a.B, a.cache.n_kv_heads, capacity);
     int32_t* starts = nullptr;
     if (a.B > kManyRequests) {
         starts = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(partial) + tiles_partial_bytes(tiles, splits, a.cache.n_kv_heads, head_dim));
         k_kv4_attention_tile_starts<<<1, kStartThreads, 0, st>>>(a, starts, small_rows);
     }
-    if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false>(a, tiles, splits, small_rows, partial, starts, st);
-        if (group == 32) return launch<64, 32, true>(a, tiles, splits, small_rows, partial, starts, st);
-        return launch<64, 64, true>(a, tiles, splits, small_rows, partial, starts, st);
-    }
-    if (group == 0) return launch<128, 128, false>(a, tiles, splits, small_rows, partial, starts, st);
-    if (group == 32) return launch<128, 32, true>(a, tiles, splits, small_rows, partial, starts, st);
-    if (group == 64) return launch<128, 64, true>(a, tiles, splits, small_rows, partial, starts, st);
-    return launch<128, 128, true>(a, tiles, splits, small_rows, partial, starts, st);
+    return masked ? launch_shape<Masked>(a, head_dim, group, tiles, splits, small_rows, partial, starts, st)
+                  : launch_shape<>(a, head_dim, group, tiles, splits, small_rows, partial, starts, st);
 }
 
 }  // namespace kv4
