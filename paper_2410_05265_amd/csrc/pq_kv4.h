@@ -102,13 +102,19 @@ int launch_tree(const int32_t* parents, const int32_t* cu_q, const int32_t* kv_l
 int launch_accept(const AcceptArgs& a, hipStream_t st);
 int launch_keep(const int64_t* from_slots, const int64_t* to_slots, int32_t B, int32_t width, const pq_kv4_cache* caches, int32_t n_caches, hipStream_t st);
 
-// capacity: tokens of a history, at most; with a window what one row and those beside it see.
-inline int64_t seen_at_most(int64_t capacity, int32_t max_q, int32_t window, int32_t sinks)
-{
-    const int64_t most = (int64_t)window + sinks + max_q + 128;
-    return most < capacity ? most : capacity;
-}
-size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity);
+// What the host knows of the histories: the table's tokens, and where kernels look at windows and trees what rows see of them.
+struct Histories {
+    int64_t table;
+    bool masked;
+    int32_t window, sinks;
+    // Tokens of one that up to `tokens` rows see, at most.
+    int64_t seen_by(int64_t tokens) const
+    {
+        const int64_t most = (int64_t)window + sinks + tokens + 128;
+        return masked && most < table ? most : table;
+    }
+};
+size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, const Histories& h);
 int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, bool masked, void* ws, hipStream_t st);
 
 }  // namespace kv4

@@ -70,9 +70,8 @@ template <int N, int M> bool any_overlap(const Range (&a)[N], const Range (&b)[M
 size_t attention_workspace(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, const pq_kv4_cache* cache, const Sight* sight)
 {
     if (check_cache_shape(cache) != PQ_OK || T <= 0 || B <= 0 || !attention_sizes_ok(T, B, n_heads, max_q, table_pages, cache)) return 0;
-    int64_t capacity = (int64_t)table_pages * cache->page_size;
-    if (sight) capacity = pq::kv4::seen_at_most(capacity, max_q, window_of(*sight), sight->sinks);
-    return pq::kv4::attention_workspace_bytes(T, B, n_heads, cache->n_kv_heads, cache->head_dim, max_q, capacity);
+    const pq::kv4::Histories h = {(int64_t)table_pages * cache->page_size, sight != nullptr, sight ? window_of(*sight) : 0, sight ? sight->sinks : 0};
+    return pq::kv4::attention_workspace_bytes(T, B, n_heads, cache->n_kv_heads, cache->head_dim, max_q, h);
 }
 
 // One call of any of the three attentions; sight null: all tokens, or with causal those up to a row's own.

@@ -832,16 +832,32 @@ int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, h
 // registers twice (16 requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
 int blocks_for(int32_t max_q, int32_t per_kv, int64_t units) { return (int64_t)max_q * per_kv > 16 && units > 48 * kGroups * kWaves ? 2 : 1; }
 
-bool takes_tiles(int32_t max_q, int32_t per_kv) { return (int64_t)max_q * per_kv > kSmallRows; }
-// A single request is the tile kernel's whatever its rows are: the two launches that would find nothing to do take 4 us (1024 tokens of one
-// prompt, 32 heads on 8: 38 us with them, 34 without).
-int small_rows_for(int32_t max_q, int32_t per_kv, int32_t B) { return !takes_tiles(max_q, per_kv) ? INT32_MAX : B > 1 ? kSmallRows : 0; }
-
-size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity)
+// The masked tile kernel cuts its work into equal runs and leaves out wavefronts without rows, so it is worth its three launches earlier, where a
+// call has much to do.  Row | tile kernel, us, trees, 32 heads of 128 on 8, with 64, 104, 128 and 192 rows: 64 requests of up to 3000 tokens 94 | 115,
+// 128 | 126, 154 | 131, 205 | 159, with a step to 32 channels 161 | 253, 238 | 266, 293 | 283, 400 | 323; 16 of 4000 46 | 54, 66 | 62, 61 | 57,
+// 74 | 66; with less to do, 4 of 4000, 29 | 35, 30 | 38, 37 | 39, 43 | 47, one of 3000 23 | 33, 26 | 36, 27 | 36, 29 | 43.
+constexpr int kMaskedSmallRows = 104;
+constexpr int64_t kMuch = 4096;          // steps of 64 tokens, of all requests and heads
+int border_for(int32_t B, int32_t n_kv_heads, int32_t per_kv, const Histories& h)
 {
-    const int small_rows = small_rows_for(max_q, n_heads / n_kv_heads, B);
+    return h.masked && (int64_t)B * n_kv_heads * h.seen_by(kSmallRows / per_kv) >= 64 * kMuch ? kMaskedSmallRows : kSmallRows;
+}
+bool takes_tiles(int32_t max_q, int32_t per_kv, int border) { return (int64_t)max_q * per_kv > border; }
+// A single request is the tile kernel's whatever its rows are: the two launches that would find nothing to do take 4 us (1024 tokens of one
+// prompt, 32 heads on 8: 38 us with them, 34 without); with the masked one, which spreads a single row's steps over all workgroups as well, also some
+// that see little, four steps to a workgroup at most.
+int small_rows_for(int32_t max_q, int32_t per_kv, int32_t B, int32_t n_kv_heads, const Histories& h)
+{
+    const int border = border_for(B, n_kv_heads, per_kv, h);
+    if (!takes_tiles(max_q, per_kv, border)) return INT32_MAX;
+    const bool little = h.masked && (int64_t)(B - 1) * n_kv_heads * h.seen_by(border / per_kv) <= 64 * 4 * 256;
+    return B == 1 || little ? 0 : border;
+}
+
+size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int small_rows, const Histories& h)
+{
     if (small_rows == 0) return 0;
-    const Most most = at_most(T, B, n_heads, n_kv_heads, capacity, small_rows);
+    const Most most = at_most(T, B, n_heads, n_kv_heads, h.seen_by(max_q), small_rows);
     return (partial_bytes(most.groups, head_dim, blocks_for(max_q, n_heads / n_kv_heads, most.units)) + (size_t)(most.items + 1) * sizeof(Item) + 255) & ~(size_t)255;
 }
 
@@ -861,23 +877,27 @@ int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int sma
 
 }  // namespace
 
-size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, int64_t capacity)
+size_t attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_q, const Histories& h)
 {
-    const size_t rows = rows_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, max_q, capacity);
-    const size_t all = rows + (takes_tiles(max_q, n_heads / n_kv_heads) ? tiles_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, capacity) : 0);
+    const int32_t per_kv = n_heads / n_kv_heads;
+    const int small_rows = small_rows_for(max_q, per_kv, B, n_kv_heads, h);
+    size_t all = rows_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, max_q, small_rows, h);
+    if (small_rows != INT32_MAX)
+        all += h.masked ? masked_tiles_workspace_bytes(T, B, per_kv, head_dim, small_rows) : tiles_workspace_bytes(T, B, n_heads, n_kv_heads, head_dim, h.table);
     return all > 256 ? all : 256;                  // (0 says that the sizes are refused)
 }
 
 int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, int32_t max_q, bool masked, void* ws, hipStream_t st)
 {
-    const int64_t table = (int64_t)a.table_pages << a.cache.log2_page, capacity = masked ? seen_at_most(table, max_q, a.window, a.sinks) : table;
-    const int small_rows = small_rows_for(max_q, a.heads_per_kv, a.B);
-    if (takes_tiles(max_q, a.heads_per_kv)) {
-        const size_t rows = rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, capacity);
-        float* const partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + rows);
-        if (const int rc = launch_attention_tiles(a, head_dim, group, small_rows, capacity, masked, partial, st); rc != PQ_OK || small_rows == 0) return rc;
+    const Histories h = {(int64_t)a.table_pages << a.cache.log2_page, masked, a.window, a.sinks};
+    const int small_rows = small_rows_for(max_q, a.heads_per_kv, a.B, a.cache.n_kv_heads, h);
+    if (small_rows != INT32_MAX) {
+        uint8_t* const partial = static_cast<uint8_t*>(ws) + rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, small_rows, h);
+        const int rc = masked ? launch_masked_tiles(a, head_dim, group, small_rows, partial, st)
+                              : launch_attention_tiles(a, head_dim, group, small_rows, reinterpret_cast<float*>(partial), st);
+        if (rc != PQ_OK || small_rows == 0) return rc;
     }
-    const int64_t units = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, capacity, small_rows).units;
+    const int64_t capacity = h.seen_by(max_q), units = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, capacity, small_rows).units;
     const bool one = blocks_for(max_q, a.heads_per_kv, units) == 1;
     if (masked) return one ? launch_rows<1, Masked>(a, head_dim, group, small_rows, capacity, ws, st) : launch_rows<2, Masked>(a, head_dim, group, small_rows, capacity, ws, st);
     return one ? launch_rows<1>(a, head_dim, group, small_rows, capacity, ws, st) : launch_rows<2>(a, head_dim, group, small_rows, capacity, ws, st);

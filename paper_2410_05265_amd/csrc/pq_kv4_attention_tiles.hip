@@ -120,6 +120,168 @@ __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index
     return {lanes(b), lanes(tile), {lanes(r.start), lanes(r.q_len), lanes(r.n), lanes(r.sees)}};
 }
 
+// ---- The masked variant's work is cut into runs.  What a tile of rows sees differs more there (windows, trees beside prompts), and so do the
+// requests: all steps of the call, request after request, in each head after head and tile of rows after tile, lie one after another, and every
+// workgroup takes an equal run of them, whatever the lengths are (a chiplet's workgroups read neighbouring rows' tokens of one head: with the
+// heads inside the tiles the codes missed its L2, prompts took 1.4 times as long).  A tile and head that a run covers whole is written as it is; of one that is cut, the workgroups leave
+// partial sums (at most two each), and a second kernel adds them.  The tiles and where the runs begin are listed by a kernel of one workgroup in
+// front: planned by every workgroup for itself they cost 40 us of code that is run once and has to come from memory.
+
+// A run is counted in units: a tile and head has one for every step and kTileUnits in front, for what it takes beside its steps (queries, prefix,
+// results; without them a run of many short tiles took up to 1.3 times as long as one of few long ones).
+constexpr int kTileUnits = 5;
+
+// A tile of rows: `steps` of 64 tokens (0: it sees nothing), of which those from Tiles::front on lie `gap` further.
+struct RowTile {
+    int b, tile, of, steps, gap;         // of: tiles of the request
+    Request r;
+};
+__device__ __forceinline__ int units_of(int steps) { return kTileUnits + max(steps, 1); }
+// Of a workgroup, its first unit: of a tile and head; tile < 0: it has none.
+struct Start {
+    int tile, head, unit, unused;
+    int64_t length, each;        // units of the run, and of one that is not the last
+};
+// A tile that was cut, by the workgroup that began it: `parts` workgroups from it on have some of it (0: none was).
+struct Cut {
+    int parts, start, rows, head, row0, unused[3];
+};
+// Runs: a workgroup to a CU, two where registers let two run there.
+template <int D, bool DYNAMIC> constexpr int kRuns = D == 64 && !DYNAMIC ? 512 : 256;
+constexpr int kMostRuns = 512, kFewestUnits = 7;
+
+// Scratch memory of the masked variant.
+struct Plan {
+    Start* starts;               // [kMostRuns]
+    Cut* cuts;                   // [kMostRuns]
+    RowTile* tiles;              // [most_tiles]
+    int64_t* units_before;       // [most_tiles + 1], of one head
+    int32_t* tiles_before;       // [B + 1], of each request
+    float* partial;              // two places for each run
+    int most_tiles;
+};
+
+// What the kernels are given beside the call's arguments: scratch memory, and how it is used.
+template <typename... KIND> struct Work {
+    float* partial;
+    const int32_t* starts;       // tiles before each request, null: not listed
+    int splits, small_rows;
+};
+template <> struct Work<Masked> {
+    Plan plan;
+};
+struct PlainParts { float* partial; const int32_t* starts; int splits, small_rows; };
+struct MaskedParts { float* partial; const Start* starts; int splits, small_rows; };
+__device__ __forceinline__ PlainParts parts_of(const Work<>& w) { return {w.partial, w.starts, w.splits, w.small_rows}; }
+__device__ __forceinline__ MaskedParts parts_of(const Work<Masked>& w) { return {w.plan.partial, w.plan.starts, 0, 0}; }
+__device__ __forceinline__ Cut* cuts_of(const Work<>&) { return nullptr; }
+__device__ __forceinline__ Cut* cuts_of(const Work<Masked>& w) { return w.plan.cuts; }
+__device__ __forceinline__ const RowTile* tiles_of(const Work<>&) { return nullptr; }
+__device__ __forceinline__ const RowTile* tiles_of(const Work<Masked>& w) { return w.plan.tiles; }
+
+// What lies there, as scalars: where a branch goes by it, and barriers stand behind the branch, the wavefronts go whole.
+template <typename T> __device__ __forceinline__ T for_all(const T* from)
+{
+    T v;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 4); ++i)
+        reinterpret_cast<int*>(&v)[i] = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(from)[i]);
+    return v;
+}
+
+constexpr int kPlanThreads = 1024;
+// Inclusive sum over the workgroup; `all`: the sum.
+__device__ __forceinline__ int64_t sum_up(int64_t v, int64_t* sums, int tid, int64_t& all)
+{
+    const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t x = __shfl_up(v, d, 64);
+        if (lane >= d) v += x;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+    all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) v += sums[w];
+        all += sums[w];
+    }
+    return v;
+}
+// The last place whose entry is at most x.
+template <typename T> __device__ __forceinline__ int place_in(const T* list, int n, int64_t x)
+{
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (list[mid] <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_kv4_attention_plan(AttentionArgs a, Plan p, int runs, int small_rows)
+{
+    __shared__ int64_t sums[kPlanThreads / 64], few_units[kPlanThreads + 1];
+    __shared__ int32_t few_tiles[kPlanThreads + 1];
+    const int tid = threadIdx.x, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv;
+    int32_t* const tiles_before = a.B <= kPlanThreads ? few_tiles : p.tiles_before;
+    const int each = (a.B + kPlanThreads - 1) / kPlanThreads, first = min(tid * each, a.B), last = min(first + each, a.B);
+    int64_t own = 0, all;
+    for (int b = first; b < last; ++b) own += tiles_of(a, request(a, b), small_rows);
+    int64_t at = sum_up(own, sums, tid, all) - own;
+    for (int b = first; b < last; ++b) {
+        tiles_before[b] = (int32_t)min(at, (int64_t)INT32_MAX);
+        if (last - first > 1) at += tiles_of(a, request(a, b), small_rows);
+    }
+    // (only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
+    const int tiles = (int)min(all, (int64_t)p.most_tiles);
+    int64_t* const units_before = tiles <= kPlanThreads ? few_units : p.units_before;
+    __syncthreads();
+    int64_t total = 0;
+    for (int t0 = 0; t0 < tiles; t0 += kPlanThreads) {
+        const int t = t0 + tid;
+        int64_t units = 0, sum;
+        if (t < tiles) {
+            // (the last of the requests that begin there: those in front of it have no tiles)
+            const int b = place_in(tiles_before, a.B, t);
+            const Request r = request(a, b);
+            const int tile = t - tiles_before[b], row0 = tile * kRows;
+            const Seen seen = masked_rows(a, r, row0 / per_kv, min((row0 + kRows - 1) / per_kv, r.q_len - 1));
+            const Tiles<kTile> left(a, seen.lo);
+            const int count = left.count(seen.any);
+            p.tiles[t] = {b, tile, tiles_of(a, r, small_rows), count, left.gap, r};
+            units = units_of(count);
+        }
+        const int64_t incl = sum_up(units, sums, tid, sum);
+        if (t < tiles) units_before[t] = total + incl - units;
+        total += sum;
+    }
+    if (tid == 0) units_before[tiles] = total;
+    __syncthreads();
+    const int64_t units = total * Hkv, length = max((units + runs - 1) / runs, (int64_t)kFewestUnits);
+    if (tid >= runs) return;
+    p.cuts[tid].parts = 0;
+    const int64_t begin = length * tid;
+    Start s = {-1, 0, 0, 0, min(length, units - begin), length};
+    if (begin < units) {
+        int lo = 0, hi = a.B - 1;                  // the request
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (units_before[min(tiles_before[mid], tiles)] * Hkv <= begin) lo = mid;
+            else hi = mid - 1;
+        }
+        const int first_tile = tiles_before[lo], end_tile = lo + 1 < a.B ? min(tiles_before[lo + 1], tiles) : tiles;
+        const int64_t base = units_before[first_tile], one = units_before[end_tile] - base, in = begin - base * Hkv;
+        s.head = (int)(in / one);
+        const int64_t at_unit = base + in - s.head * one;
+        s.tile = first_tile + place_in(units_before + first_tile, end_tile - first_tile, at_unit);
+        s.unit = (int)(at_unit - units_before[s.tile]);
+    }
+    p.starts[tid] = s;
+}
+
 // Row `at` of the accumulators as a channel: channels of a group lie so in LDS that neighbouring threads of the expansion write
 // neighbouring places.
 template <int G> __device__ __forceinline__ constexpr int channel_of(int at)
@@ -157,35 +319,108 @@ struct Lds {
 // static steps, 32 heads on 8, one | two: 4 prompts of up to 4096 tokens 232 | 206 us, 4 of 4096 390 | 357, 300 queries each over up to 4000 64 |
 // 65, 500 over 33000 178 | 184; with dynamic steps what does not fit is spilled: to 64 channels 347 | 422, 500 over 33000 277 | 531).
 template <int D, int G, bool DYNAMIC, typename... KIND>
-__global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs a, float* partial, const int32_t* __restrict__ starts, int splits, int small_rows)
+__global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_attention_tiles(AttentionArgs given, Work<KIND...> work)
 {
     constexpr bool MASKED = sizeof...(KIND) > 0;
+    [[maybe_unused]] const auto [partial, starts, splits, small_rows] = parts_of(work);
     constexpr int NG = D / G, KS = D / 16, KSG = G / 16, DB = D / 32, DBG = G / 32;
     extern __shared__ __align__(256) uint8_t raw_lds[];
     typedef Lds<D, G, DYNAMIC> L;
     L& sh = *reinterpret_cast<L*>(raw_lds);
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 31, half = lane >> 5;
-    const int log2_page = a.cache.log2_page, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv;
-    const int head = blockIdx.x % Hkv, split = (blockIdx.x / Hkv) % splits;
-    const int64_t index = blockIdx.x / Hkv / splits;
-    const Where at = find_tile(a, index, small_rows, starts, lane);
-    if (at.b < 0) return;
+    const int worker = MASKED ? xcd_run(blockIdx.x, gridDim.x) : 0;
+    [[maybe_unused]] Cut* const cuts = cuts_of(work);
+    [[maybe_unused]] const RowTile* const row_tiles = tiles_of(work);
+    // Codes on their way run from one tile of rows into the next: where the steps of the one and the other find theirs.
+    struct Source {
+        const int32_t* table;
+        int head, n, gap, unused;
+    };
+    // What a wavefront keeps from tile to tile.  It lies in LDS, for each of its own: the compiler orders loads and products by the registers that are
+    // left, and with this in scalar ones it read every operand right in front of its product (a step of 2.1 us took 2.5).
+    struct Held {
+        Start run;
+        RowTile tile;            // what comes then
+        Source now, then;
+    };
+    __shared__ Held held_by[kWaves];
+    if constexpr (MASKED) {
+        Held& held = held_by[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
+        const Start run = for_all(starts + worker);
+        if (run.tile < 0) return;
+        held.run = run;
+        held.tile = for_all(row_tiles + run.tile);
+    }
+    struct Codes { v4u w; float s; int bad, left; };               // left: tokens from the tile's first on
+    Codes next;
+    int page = 0, first_buf = 0;
+    bool primed = false, ahead = false;
+    while (true) {
+    // (read anew for every tile of rows: kept, the arguments alone take half of the scalar registers)
+    auto arguments = [&]() PQ_INLINE -> const AttentionArgs& {
+        if constexpr (!MASKED) return given;
+        uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(at));
+        return *(const AttentionArgs*)(const __attribute__((address_space(4))) AttentionArgs*)at;
+    };
+    const AttentionArgs& a = arguments();
+    const int log2_page = a.cache.log2_page, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv, left_front = MASKED ? Tiles<kTile>(a, 0).front : 0;
+    int tid = threadIdx.x;
+    if constexpr (MASKED) asm volatile("" : "+v"(tid));            // (what comes from it is not kept from one tile to the next: registers)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    int head = blockIdx.x % Hkv, split = MASKED ? 0 : (blockIdx.x / Hkv) % splits, begin, end;
+    const int64_t index = MASKED ? 0 : blockIdx.x / Hkv / splits;
+    bool cut = MASKED ? false : splits > 1;        // its sums go through scratch memory
+    Where at;
+    int more_units = 0, next_index = 0, next_head = 0, gap = 0;
+    Held& held = held_by[wave];
+    if constexpr (MASKED) {
+        Start run = for_all(&held.run);
+        const RowTile row_tile = for_all(&held.tile);
+        if (run.length <= 0) return;
+        if (!primed) __syncthreads();              // (nobody reads the last tile's operands any more)
+        at = {row_tile.b, row_tile.tile, row_tile.r};
+        head = run.head;
+        const int units = units_of(row_tile.steps), take = (int)min((int64_t)(units - run.unit), run.length), last = run.unit + take;
+        if (last <= kTileUnits) return;            // (the run ends in front of its first step)
+        begin = max(run.unit - kTileUnits, 0);
+        end = min(last - kTileUnits, row_tile.steps);
+        cut = begin > 0 || last < units;
+        split = begin;
+        held.now = {a.table + (int64_t)at.b * a.table_pages, head, at.r.n, row_tile.gap, 0};
+        if (begin == 0 && cut && tid == 0) {
+            int parts = 1;
+            for (int64_t left = units - last; left > 0; left -= run.each) ++parts;
+            cuts[worker] = {parts, at.r.start, at.r.q_len * per_kv, head, at.tile * kRows, {0, 0, 0}};
+        }
+        run.length -= take;
+        run.unit = 0;
+        ++run.tile;
+        if (row_tile.tile + 1 == row_tile.of && run.head + 1 < Hkv) {
+            ++run.head;
+            run.tile -= row_tile.of;
+        } else if (row_tile.tile + 1 == row_tile.of) {
+            run.head = 0;
+        }
+        held.run = run;
+        more_units = (int)min(run.length, (int64_t)kTileUnits + 1);
+        next_index = run.tile;
+        next_head = run.head;
+        gap = row_tile.gap;
+    } else {
+        at = find_tile(a, index, small_rows, starts, lane);
+        if (at.b < 0) return;
+    }
     const Request r = at.r;
     const int rows = r.q_len * per_kv, row0 = at.tile * kRows;
-    const int last_token = min((row0 + kRows - 1) / per_kv, r.q_len - 1);
     const bool tree = MASKED && is_tree(a, r);
-    int lo = 0;                                    // no row sees a token before it that is no sink
-    int visible = __builtin_amdgcn_readfirstlane(sees(a, r, last_token));              // (a division leaves it in a vector register)
-    if constexpr (MASKED) {
-        const Seen seen = masked_rows(a, r, row0 / per_kv, last_token);
-        visible = __builtin_amdgcn_readfirstlane(seen.any);
-        lo = __builtin_amdgcn_readfirstlane(seen.lo);
+    const bool live = !MASKED || row0 + wave * kCols < rows;      // some of the wavefront's rows are there
+    if constexpr (!MASKED) {
+        const int last_token = min((row0 + kRows - 1) / per_kv, r.q_len - 1);
+        const int visible = __builtin_amdgcn_readfirstlane(sees(a, r, last_token));    // (a division leaves it in a vector register)
+        const int all_tiles = (visible + kTile - 1) / kTile;
+        begin = (int)((int64_t)all_tiles * split / splits);
+        end = (int)((int64_t)all_tiles * (split + 1) / splits);
     }
-    const Tiles<kTile> left_in(a, lo);
-    auto tile_at = [&](int i) PQ_INLINE -> int { return MASKED ? left_in.at(i) : i; };
-    const int all_tiles = MASKED ? left_in.count(visible) : (visible + kTile - 1) / kTile;
-    const int begin = (int)((int64_t)all_tiles * split / splits), end = (int)((int64_t)all_tiles * (split + 1) / splits);
 
     // this lane's query
     int limit, wave_sees;                    // tokens that it sees, and that all of the wavefront's see
@@ -211,16 +446,24 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8h*>(src + 16 * s + 8 * half);
     }
+    // What a tile of rows needs beside the steps is asked for at once: queries, prefix tokens, pages, the tile that comes then.  One after another
+    // these waits took as long as two steps.
+    // ---- prefix tokens, in tiles of 32: a thread's token and eight channels of it
+    const bool prefix = a.n_prefix > 0 && split == 0;
+    const int prefix_t = tid / (D / 8), prefix_c = tid % (D / 8);
+    v4u prefix_k = {}, prefix_v = {};
+    auto load_prefix = [&](int t0) PQ_INLINE {
+        if (prefix_t >= kPrefixTile) return;
+        const int64_t from = ((int64_t)min(t0 + prefix_t, a.n_prefix - 1) * Hkv + head) * D + 8 * prefix_c;
+        prefix_k = *reinterpret_cast<const v4u*>(a.prefix_k + from);
+        prefix_v = *reinterpret_cast<const v4u*>(a.prefix_v + from);
+    };
+    if (prefix) load_prefix(0);
+
     // ---- the history: wavefronts w and w + 4 load and expand keys and values of tokens 16 w .. 16 w + 15 of every tile
-    const int32_t* table = a.table + (int64_t)at.b * a.table_pages;
     const int block = wave & 3;
     const bool keys = wave < 4;
-    struct Codes { v4u w; float s; int bad; };
-    auto page_of = [&](int tile) PQ_INLINE { return table[min((tile * kTile + 16 * block) >> log2_page, a.table_pages - 1)]; };
-    auto load = [&](int tile, int page, Codes& x) PQ_INLINE {
-        const int t = tile * kTile + 16 * block;
-        x.bad = (uint32_t)page >= (uint64_t)a.cache.n_pages || (t >> log2_page) >= a.table_pages;
-        const int64_t from = x.bad ? 0 : page, first = ((from * Hkv + head) << log2_page) + (t & ((1 << log2_page) - 1));
+    auto fetch = [&](int64_t first, Codes& x) PQ_INLINE {          // 16 tokens from this one of the head's on
         // (one vector, set as a whole on both sides: an array's members went through scratch memory in every step)
         if (keys) {                                // D / 4 channels of a token to a lane
             const uint8_t* src = a.cache.k_codes + (first + (lane >> 2)) * (D / 2) + (lane & 3) * (D / 8);
@@ -242,7 +485,54 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             if ((lane & 3) < NG) x.s = (keys ? a.cache.k_scale : a.cache.v_scale)[(first + (lane >> 2)) * NG + (lane & 3)];
         }
     };
-    auto expand = [&](int tile, int buf, const Codes& x) PQ_INLINE {
+    const int32_t* const table = a.table + (int64_t)at.b * a.table_pages;
+    auto page_of = [&](int tile) PQ_INLINE { return table[min((tile * kTile + 16 * block) >> log2_page, a.table_pages - 1)]; };
+    auto load = [&](int tile, int page, Codes& x) PQ_INLINE {
+        const int t = tile * kTile + 16 * block;
+        x.bad = (uint32_t)page >= (uint64_t)a.cache.n_pages || (t >> log2_page) >= a.table_pages;
+        x.left = r.n - tile * kTile;
+        const int64_t from = x.bad ? 0 : page;
+        fetch(((from * Hkv + head) << log2_page) + (t & ((1 << log2_page) - 1)), x);
+    };
+    // MASKED: step i is tile i, or lies behind the gap; steps from `end` on are the next item's first two.  64 pages are looked up at once, and a lane
+    // read where one is used.  (A page carried from step to step through the outer loop was waited for at once, and what is computed for every step
+    // is kept short: twice the scalar instructions made a step of 2.1 us 2.6.)
+    int load_tile = 0, ids_from = 0;               // the last tile that is on its way; slots of pages from ids_from on, and which are none
+    int64_t slots = 0;
+    uint64_t none = 0;
+    int then_page = 0;                             // lanes 0 and 1: of the next item's first two steps
+    auto tile_of = [&](int step, int gap) PQ_INLINE { return step + (step >= left_front ? gap : 0); };
+    auto page_at = [&](int tile) PQ_INLINE { return (tile * kTile + 16 * block) >> log2_page; };
+    auto look_up = [&](int from, int page, int head) PQ_INLINE {
+        const int at = from + lane;
+        const bool bad = (uint32_t)page >= (uint64_t)a.cache.n_pages || at >= a.table_pages;
+        slots = ((int64_t)(bad ? 0 : page) * Hkv + head) << log2_page;
+        none = __builtin_amdgcn_ballot_w64(bad);
+        ids_from = from;
+    };
+    auto load_step = [&](int i, Codes& x) PQ_INLINE {
+        const int in = (1 << log2_page) - 1;
+        if (i >= end) {
+            if (!ahead) return;                    // (nothing comes then)
+            const Source then = for_all(&held.then);
+            const int tile = tile_of(i - end, then.gap), page = __builtin_amdgcn_readlane(then_page, i - end);
+            x.bad = (uint32_t)page >= (uint64_t)a.cache.n_pages || page_at(tile) >= a.table_pages;
+            x.left = then.n - tile * kTile;
+            fetch(((int64_t)((x.bad ? 0 : page) * (int64_t)Hkv + then.head) << log2_page) + ((tile * kTile + 16 * block) & in), x);
+            return;
+        }
+        load_tile = i == left_front ? i + gap : load_tile + 1;
+        const int at = page_at(load_tile);
+        if ((uint32_t)(at - ids_from) >= 64) {
+            const Source now = for_all(&held.now);
+            look_up(at, now.table[min(at + lane, a.table_pages - 1)], now.head);
+        }
+        x.bad = (int)(none >> (at - ids_from)) & 1;
+        x.left = r.n - load_tile * kTile;
+        const uint32_t low = __builtin_amdgcn_readlane((int)(uint32_t)slots, at - ids_from), high = __builtin_amdgcn_readlane((int)(slots >> 32), at - ids_from);
+        fetch((int64_t)((uint64_t)high << 32 | low) + ((load_tile * kTile + 16 * block) & in), x);
+    };
+    auto expand = [&](int buf, const Codes& x) PQ_INLINE {
         const int t = 16 * block + (lane >> 2);
         if (keys) {
 #pragma unroll
@@ -270,7 +560,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             if constexpr (DYNAMIC) {
                 // what lies behind the last token, or in no page, may be anything, and what only later queries see may be infinite: neither
                 // must meet a probability of zero as it is
-                const float step = tile * kTile + t < r.n && !x.bad ? finite_step(x.s) : 0.0f;
+                const float step = t < x.left && !x.bad ? finite_step(x.s) : 0.0f;
                 float most = step;
 #pragma unroll
                 for (int d = 4; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
@@ -280,24 +570,26 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
         }
     };
 
-    Codes next;
-    int page = 0;
-    if (begin < end) {                             // (on their way while the queries are and the prefix tokens are taken)
-        load(tile_at(begin), page_of(tile_at(begin)), next);
-        page = page_of(tile_at(begin + 1));
+    if constexpr (MASKED) {
+        load_tile = tile_of(begin + (primed ? 1 : 0), gap) - (primed ? 0 : 1);
+        const int from = max(page_at(load_tile), 0), page = begin < end ? table[min(from + lane, a.table_pages - 1)] : 0;
+        RowTile next_tile = {};
+        if (more_units > 0) next_tile = for_all(row_tiles + next_index);
+        held.tile = next_tile;
+        look_up(from, page, head);
+        // the last steps load the first two of the next tile's
+        ahead = end - begin >= 2 && more_units > kTileUnits && next_tile.steps > 0;
+        if (begin < end && !primed) load_step(begin, next);
+        if (ahead) {
+            const int32_t* const then_table = a.table + (int64_t)next_tile.b * a.table_pages;
+            held.then = {then_table, next_head, next_tile.r.n, next_tile.gap, 0};
+            then_page = then_table[min(page_at(tile_of(lane & 1, next_tile.gap)), a.table_pages - 1)];
+        }
+    } else if (begin < end) {                      // (on their way while the queries are and the prefix tokens are taken)
+        load(begin, page_of(begin), next);
+        page = page_of(begin + 1);
     }
 
-    // ---- prefix tokens, in tiles of 32: a thread's token and eight channels of it
-    const bool prefix = a.n_prefix > 0 && split == 0;
-    const int prefix_t = tid / (D / 8), prefix_c = tid % (D / 8);
-    v4u prefix_k = {}, prefix_v = {};
-    auto load_prefix = [&](int t0) PQ_INLINE {
-        if (prefix_t >= kPrefixTile) return;
-        const int64_t from = ((int64_t)min(t0 + prefix_t, a.n_prefix - 1) * Hkv + head) * D + 8 * prefix_c;
-        prefix_k = *reinterpret_cast<const v4u*>(a.prefix_k + from);
-        prefix_v = *reinterpret_cast<const v4u*>(a.prefix_v + from);
-    };
-    if (prefix) load_prefix(0);
 
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = in_key_order(__builtin_bit_cast(v4u, q[s]));
@@ -431,35 +723,37 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     };
 
     // ---- prefix tokens, in fp16 where the codes' operands lie
+    const int spare = MASKED && primed ? first_buf ^ 1 : 0;       // (the other one holds the first tile)
     if (prefix) {
         for (int t0 = 0; t0 < a.n_prefix; t0 += kPrefixTile) {
             __syncthreads();
             if (prefix_t < kPrefixTile) {
                 const int t = prefix_t, in16 = t & 15;             // token t of its 16: 8 (t / 8) + 4 (half of the lanes) + t % 4
-                sh.k[0][t][prefix_c] = __builtin_bit_cast(v4u, in_key_order(prefix_k));
+                sh.k[spare][t][prefix_c] = __builtin_bit_cast(v4u, in_key_order(prefix_k));
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    __half* dst = reinterpret_cast<__half*>(&sh.v[0][t >> 4][(in16 >> 2) & 1][place_of<G>(8 * prefix_c + j)][in16 >> 3]);
+                    __half* dst = reinterpret_cast<__half*>(&sh.v[spare][t >> 4][(in16 >> 2) & 1][place_of<G>(8 * prefix_c + j)][in16 >> 3]);
                     dst[in16 & 3] = reinterpret_cast<const __half*>(&prefix_v)[j];
                 }
             }
             if constexpr (DYNAMIC) {
                 if (tid < kPrefixTile) {
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) sh.ks[0][g][tid] = 1.0f;
+                    for (int g = 0; g < NG; ++g) sh.ks[DYNAMIC ? spare : 0][g][tid] = 1.0f;
                 }
             }
             if (t0 + kPrefixTile < a.n_prefix) load_prefix(t0 + kPrefixTile);
             __syncthreads();
             float x[kPrefixTile / 2];
             v4u p[kPrefixTile / 16];
-            scores(0, x);
+            if (MASKED && !live) continue;
+            scores(spare, x);
             const int left = a.n_prefix - t0 - 4 * half;
 #pragma unroll
             for (int i = 0; i < kPrefixTile / 2; ++i)
                 if (8 * (i >> 2) + (i & 3) >= left) x[i] = -INFINITY;
             probabilities(x, scale, 0.0f, p);
-            multiply(0, 0, DB, p);
+            multiply(spare, 0, DB, p);
         }
         __syncthreads();
         // in units of a code
@@ -474,36 +768,49 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
 
     if (begin < end) {
         const float bias = c0 * c1;
-        expand(tile_at(begin), 0, next);
-        load(tile_at(begin + 1), page, next);
-        page = page_of(tile_at(begin + 2));
+        if constexpr (!MASKED) {
+            expand(0, next);
+            load(begin + 1, page, next);
+            page = page_of(begin + 2);
+        } else if (!primed) {
+            first_buf = 0;
+            expand(0, next);
+            load_step(begin + 1, next);
+        }
+        int tile = MASKED ? tile_of(begin, gap) - 1 : begin - 1;
+        auto history = [&](auto live_rows) PQ_INLINE {
+        constexpr bool LIVE = decltype(live_rows)::value;          // (else the wavefront only loads and expands for the others)
         for (int i = begin; i < end; ++i) {
-            const int buf = (i - begin) & 1;
+            const int buf = (MASKED ? first_buf + i - begin : i - begin) & 1;
             __syncthreads();                       // tile i is in LDS; nobody reads tile i - 1 any more
-            const int page_after = page_of(tile_at(i + 3)), t0 = tile_at(i) * kTile;
+            const int page_after = MASKED ? 0 : page_of(i + 3);
+            tile = MASKED && i == left_front ? i + gap : tile + 1;
+            const int t0 = tile * kTile;
             float x[32];
             v4u p[4];
-            scores(buf, x);
-            expand(tile_at(i + 1), buf ^ 1, next);
-            load(tile_at(i + 2), page, next);
+            if constexpr (LIVE) scores(buf, x);
+            expand(buf ^ 1, next);
+            if constexpr (MASKED) load_step(i + 2, next);
+            else load(i + 2, page, next);
             page = page_after;
+            if constexpr (!LIVE) continue;
             // what rows do not see, or has no page
             if (t0 + kTile > wave_sees || (MASKED && t0 < wave_hidden && t0 + kTile > a.sinks) ||
                 __builtin_amdgcn_readfirstlane(sh.bad[buf][0] | sh.bad[buf][1] | sh.bad[buf][2] | sh.bad[buf][3]) != 0) {
                 const int left = limit - (t0 + 4 * half);
-                if constexpr (MASKED) {
-                    uint32_t nodes[2] = {0, 0};    // of the tree, tokens that the query sees behind its limit
-                    if (tree && t0 + kTile > wave_sees) {
-                        nodes[0] = mask_bits(a, r, row_token, t0 - (r.sees - 1)) >> (4 * half);
-                        nodes[1] = mask_bits(a, r, row_token, t0 + 32 - (r.sees - 1)) >> (4 * half);
+                if constexpr (MASKED) {            // a bit for each of 64 tokens from this lane's first on (a branch for every score took 2 us)
+                    auto below = [](int n) PQ_INLINE -> uint64_t { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; };
+                    uint64_t see = below(left) & (~below(hidden - (t0 + 4 * half)) | below(a.sinks - (t0 + 4 * half)));
+                    if (tree && t0 + kTile > wave_sees) {          // nodes of its mask, behind the limit
+                        const uint32_t low = mask_bits(a, r, row_token, t0 - (r.sees - 1)), high = mask_bits(a, r, row_token, t0 + 32 - (r.sees - 1));
+                        see |= (((uint64_t)high << 32 | low) >> (4 * half)) & ~below(left);
                     }
-                    const int from = hidden - (t0 + 4 * half), front = a.sinks - (t0 + 4 * half);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int at = 8 * (j >> 2) + (j & 3);
-                        const bool sees_it = at < left ? at >= from || at < front : (nodes[at >> 5] >> (at & 31)) & 1;
-                        if (!sees_it || sh.bad[buf][j >> 3]) x[j] = -INFINITY;
-                    }
+                    for (int k = 0; k < 4; ++k)
+                        if (sh.bad[buf][k]) see &= ~(0xFFFFull << (16 * k));
+                    const uint32_t see_low = (uint32_t)see, see_high = (uint32_t)(see >> 32);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = ((j < 16 ? see_low : see_high) >> ((8 * (j >> 2) + (j & 3)) & 31)) & 1 ? x[j] : -INFINITY;
                 } else {
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
@@ -525,6 +832,17 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
                 multiply(buf, 0, DB, p);
             }
         }
+        };
+        if constexpr (MASKED) {
+            if (live) history(std::true_type{});
+            else history(std::false_type{});
+            first_buf = (first_buf + end - begin) & 1;
+            primed = ahead;
+        } else {
+            history(std::true_type{});
+        }
+    } else if constexpr (MASKED) {
+        primed = false;
     }
 
     // ---- results
@@ -532,9 +850,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
     float times[NG];
 #pragma unroll
     for (int g = 0; g < NG; ++g) times[g] = kUnit * (DYNAMIC ? ref[g] : v_step);
-    if (splits > 1) {
+    if (cut) {
         // [slot][row of the accumulators, maximum, sum][256 rows]: neighbouring lanes write neighbouring floats
-        float* dst = partial + ((index * Hkv + head) * splits + split) * (int64_t)(D + 2) * kRows + wave * kCols + col;
+        if (MASKED && !live) continue;
+        float* dst = partial + (MASKED ? 2 * worker + (split == 0 ? 1 : 0) : (index * Hkv + head) * splits + split) * (int64_t)(D + 2) * kRows + wave * kCols + col;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -544,10 +863,11 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             dst[D * kRows] = m;
             dst[(D + 1) * kRows] = l_all;
         }
+        if constexpr (MASKED) continue;
         return;
     }
-    __syncthreads();
-    __half* const lines = reinterpret_cast<__half*>(raw_lds) + wave * kCols * (D + 8);
+    if constexpr (!MASKED) __syncthreads();
+    __half* const lines = reinterpret_cast<__half*>(raw_lds + (MASKED ? sizeof(L) : 0)) + wave * kCols * (D + 8);      // (the next tile's operands may be there)
     const float f = l_all > 0.0f ? 1.0f / l_all : 0.0f;
     if constexpr (G >= 64) {                       // a lane holds eight channels in a row, 16 bytes
         constexpr int kStep = G / 8, kOver = 16 / kStep;           // rows of the accumulators between them, of them in one block
@@ -583,6 +903,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
         if (row < rows)
             *reinterpret_cast<v4u*>(a.out + ((int64_t)(r.start + row / per_kv) * a.n_heads + head * per_kv + row % per_kv) * D + 8 * (lane % kPer)) =
                 *reinterpret_cast<const v4u*>(lines + i * (D + 8) + 8 * (lane % kPer));
+    }
+    if constexpr (!MASKED) return;
     }
 }
 
@@ -625,6 +947,60 @@ __global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_tiles(Atten
     }
 }
 
+// The same for the tiles that runs have cut: a workgroup takes 64 rows and 64 channels of one, a thread 16 channels of a row.  The loads of four
+// parts are on their way at once (one after another, and 32 channels to a thread: 10 tiles of rows x 8 heads in four parts each 32 us).
+template <int D, int G>
+__global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_runs(AttentionArgs a, Plan p)
+{
+    constexpr int kAtOnce = 4, kChannels = 16;
+    const Cut cut = p.cuts[blockIdx.x];
+    const int lane = threadIdx.x & 63, in_tile = blockIdx.y * 64 + lane, row = cut.row0 + in_tile;
+    if (cut.parts <= 0 || cut.row0 + (int)blockIdx.y * 64 >= cut.rows) return;
+    const int channel0 = blockIdx.z * 64 + kChannels * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // part 0 lies at its workgroup's second place, the others at the first of theirs
+    const int64_t size = (int64_t)(D + 2) * kRows;
+    const float* const first = p.partial + blockIdx.x * 2 * size + in_tile;
+    float top = kNothing, sum = 0.0f, acc[kChannels] = {};
+    for (int s0 = 0; s0 < cut.parts; s0 += kAtOnce) {
+        float m[kAtOnce], l[kAtOnce], x[kAtOnce][kChannels];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int s = min(s0 + k, cut.parts - 1);
+            const float* const src = first + (2 * s + (s == 0 ? 1 : 0)) * size;
+            m[k] = src[D * kRows];
+            l[k] = src[(D + 1) * kRows];
+            if (s0 + k >= cut.parts) l[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kChannels; ++i) x[k][i] = src[place_of<G>(channel0 + i) * kRows];
+        }
+        float to = top;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) to = fmaxf(to, m[k]);
+        const float old = __builtin_amdgcn_exp2f(top - to);
+        top = to;
+        sum *= old;
+#pragma unroll
+        for (int i = 0; i < kChannels; ++i) acc[i] *= old;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float f = s0 + k < cut.parts ? __builtin_amdgcn_exp2f(m[k] - to) : 0.0f;
+            sum = fmaf(l[k], f, sum);
+#pragma unroll
+            for (int i = 0; i < kChannels; ++i) acc[i] = fmaf(x[k][i], f, acc[i]);
+        }
+    }
+    if (row >= cut.rows) return;
+    const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+    __half* const dst = a.out + ((int64_t)(cut.start + row / a.heads_per_kv) * a.n_heads + cut.head * a.heads_per_kv + row % a.heads_per_kv) * D + channel0;
+#pragma unroll
+    for (int i = 0; i < kChannels; i += 8) {
+        v4u w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = two_halves(acc[i + 2 * j] * f, acc[i + 2 * j + 1] * f);
+        *reinterpret_cast<v4u*>(dst + i) = w;
+    }
+}
+
 // Tiles of rows, at most.  Of several requests only those of more than 192 rows come here, and R such rows are at most 2 R / 257 tiles
 // (two of 257): requests that decode beside a prompt do not count as a tile each.
 int64_t tiles_at_most(int64_t T, int32_t B, int32_t per_kv)
@@ -658,15 +1034,32 @@ int splits_for(int64_t tiles, int32_t B, int32_t n_kv_heads, int64_t capacity)
 }
 
 template <int D, int G, bool DYNAMIC, typename... KIND>
-int launch(const AttentionArgs& a, int64_t tiles, int splits, int small_rows, float* partial, const int32_t* starts, hipStream_t st)
+int launch(const AttentionArgs& a, int64_t groups, const Work<KIND...>& work, hipStream_t st)
 {
     static std::atomic<uint64_t> allowed{0};
-    const size_t out = (size_t)kWaves * kCols * (D + 8) * 2, lds = sizeof(Lds<D, G, DYNAMIC>) > out ? sizeof(Lds<D, G, DYNAMIC>) : out;
+    const size_t out = (size_t)kWaves * kCols * (D + 8) * 2, in = sizeof(Lds<D, G, DYNAMIC>), lds = sizeof...(KIND) > 0 ? in + out : in > out ? in : out;
     const auto kernel = k_kv4_attention_tiles<D, G, DYNAMIC, KIND...>;
     if (const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds, allowed); rc != PQ_OK) return rc;
-    const int Hkv = a.cache.n_kv_heads;
-    kernel<<<(unsigned)(tiles * Hkv * splits), kThreads, lds, st>>>(a, partial, starts, splits, small_rows);
-    if (splits > 1) k_kv4_attention_join_tiles<D, G><<<dim3((unsigned)(tiles * Hkv), kRows / 64), kJoinThreads, 0, st>>>(a, partial, starts, splits, small_rows);
+    kernel<<<(unsigned)groups, kThreads, lds, st>>>(a, work);
+    return hip_status(hipGetLastError());
+}
+
+template <int D, int G, bool DYNAMIC>
+int launch_plain(const AttentionArgs& a, int64_t groups, const Work<>& work, hipStream_t st)
+{
+    if (const int rc = launch<D, G, DYNAMIC>(a, groups * work.splits, work, st); rc != PQ_OK) return rc;
+    if (work.splits > 1)
+        k_kv4_attention_join_tiles<D, G><<<dim3((unsigned)groups, kRows / 64), kJoinThreads, 0, st>>>(a, work.partial, work.starts, work.splits, work.small_rows);
+    return hip_status(hipGetLastError());
+}
+
+template <int D, int G, bool DYNAMIC>
+int launch_masked(const AttentionArgs& a, int small_rows, const Work<Masked>& work, hipStream_t st)
+{
+    constexpr int runs = kRuns<D, DYNAMIC>;
+    k_kv4_attention_plan<<<1, kPlanThreads, 0, st>>>(a, work.plan, runs, small_rows);
+    if (const int rc = launch<D, G, DYNAMIC, Masked>(a, runs, work, st); rc != PQ_OK) return rc;
+    k_kv4_attention_join_runs<D, G><<<dim3(runs, kRows / 64, D / 64), kJoinThreads, 0, st>>>(a, work.plan);
     return hip_status(hipGetLastError());
 }
 
@@ -676,21 +1069,57 @@ size_t tiles_partial_bytes(int64_t tiles, int splits, int32_t n_kv_heads, int32_
     return splits > 1 ? (size_t)(tiles * n_kv_heads * splits) * kRows * (head_dim + 2) * sizeof(float) : 0;
 }
 
-template <typename... KIND>
-int launch_shape(const AttentionArgs& a, int32_t head_dim, int32_t group, int64_t tiles, int splits, int small_rows, float* partial, const int32_t* starts, hipStream_t st)
+// Of the masked variant, with requests of more than small_rows rows: 256 rows of one at least, or the rows of a smaller one.
+int64_t masked_tiles_at_most(int64_t T, int32_t B, int32_t per_kv, int small_rows)
 {
-    if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
-        if (group == 32) return launch<64, 32, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
-        return launch<64, 64, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
-    }
-    if (group == 0) return launch<128, 128, false, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
-    if (group == 32) return launch<128, 32, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
-    if (group == 64) return launch<128, 64, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
-    return launch<128, 128, true, KIND...>(a, tiles, splits, small_rows, partial, starts, st);
+    const int64_t rows = T * per_kv, by_requests = rows / kRows + B, fewest = small_rows + 1 < (kRows + 1) / 2 ? small_rows + 1 : (kRows + 1) / 2;
+    const int64_t by_rows = rows / fewest + 1;
+    return by_requests < by_rows ? by_requests : by_rows;
+}
+
+size_t up_to_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+// The masked variant's scratch memory, at `ws`; its size.
+size_t lay_out(Plan* p, void* ws, int64_t most_tiles, int32_t B, int32_t head_dim)
+{
+    uint8_t* const base = static_cast<uint8_t*>(ws);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up_to_256(bytes);
+        return base + here;
+    };
+    p->starts = reinterpret_cast<Start*>(take(kMostRuns * sizeof(Start)));
+    p->cuts = reinterpret_cast<Cut*>(take(kMostRuns * sizeof(Cut)));
+    p->tiles = reinterpret_cast<RowTile*>(take((size_t)most_tiles * sizeof(RowTile)));
+    p->units_before = reinterpret_cast<int64_t*>(take(most_tiles > kPlanThreads ? (size_t)(most_tiles + 1) * sizeof(int64_t) : 0));
+    p->tiles_before = reinterpret_cast<int32_t*>(take(B > kPlanThreads ? (size_t)(B + 1) * sizeof(int32_t) : 0));
+    p->partial = reinterpret_cast<float*>(take((size_t)(head_dim == 64 ? kMostRuns : 256) * 2 * kRows * (head_dim + 2) * sizeof(float)));
+    p->most_tiles = (int)most_tiles;
+    return at;
 }
 
 }  // namespace
+
+size_t masked_tiles_workspace_bytes(int64_t T, int32_t B, int32_t per_kv, int32_t head_dim, int small_rows)
+{
+    Plan p;
+    return lay_out(&p, nullptr, masked_tiles_at_most(T, B, per_kv, small_rows), B, head_dim);
+}
+
+int launch_masked_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, void* ws, hipStream_t st)
+{
+    Work<Masked> w;
+    lay_out(&w.plan, ws, masked_tiles_at_most(a.T, a.B, a.heads_per_kv, small_rows), a.B, head_dim);
+    if (head_dim == 64) {
+        if (group == 0) return launch_masked<64, 64, false>(a, small_rows, w, st);
+        if (group == 32) return launch_masked<64, 32, true>(a, small_rows, w, st);
+        return launch_masked<64, 64, true>(a, small_rows, w, st);
+    }
+    if (group == 0) return launch_masked<128, 128, false>(a, small_rows, w, st);
+    if (group == 32) return launch_masked<128, 32, true>(a, small_rows, w, st);
+    if (group == 64) return launch_masked<128, 64, true>(a, small_rows, w, st);
+    return launch_masked<128, 128, true>(a, small_rows, w, st);
+}
 
 size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity)
 {
@@ -699,17 +1128,26 @@ size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv
     return tiles_partial_bytes(tiles, splits, n_kv_heads, head_dim) + (B > kManyRequests ? ((size_t)(B + 1) * sizeof(int32_t) + 255) & ~(size_t)255 : 0);
 }
 
-int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, int64_t capacity, bool masked, float* partial, hipStream_t st)
+int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st)
 {
     const int64_t tiles = tiles_at_most(a.T, a.B, a.heads_per_kv);
-    const int splits = splits_for(tiles, a.B, a.cache.n_kv_heads, capacity);
+    const int splits = splits_for(tiles, a.B, a.cache.n_kv_heads, (int64_t)a.table_pages << a.cache.log2_page);
     int32_t* starts = nullptr;
     if (a.B > kManyRequests) {
         starts = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(partial) + tiles_partial_bytes(tiles, splits, a.cache.n_kv_heads, head_dim));
         k_kv4_attention_tile_starts<<<1, kStartThreads, 0, st>>>(a, starts, small_rows);
     }
-    return masked ? launch_shape<Masked>(a, head_dim, group, tiles, splits, small_rows, partial, starts, st)
-                  : launch_shape<>(a, head_dim, group, tiles, splits, small_rows, partial, starts, st);
+    const int64_t groups = tiles * a.cache.n_kv_heads;
+    const Work<> w = {partial, starts, splits, small_rows};
+    if (head_dim == 64) {
+        if (group == 0) return launch_plain<64, 64, false>(a, groups, w, st);
+        if (group == 32) return launch_plain<64, 32, true>(a, groups, w, st);
+        return launch_plain<64, 64, true>(a, groups, w, st);
+    }
+    if (group == 0) return launch_plain<128, 128, false>(a, groups, w, st);
+    if (group == 32) return launch_plain<128, 32, true>(a, groups, w, st);
+    if (group == 64) return launch_plain<128, 64, true>(a, groups, w, st);
+    return launch_plain<128, 128, true>(a, groups, w, st);
 }
 
 }  // namespace kv4

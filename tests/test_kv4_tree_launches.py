@@ -47,7 +47,9 @@ def test_attention_takes_the_kernels_of_its_kind(fn):
     for D, group in ((64, 0), (64, 32), (64, 64), (128, 0), (128, 32), (128, 64), (128, 128)):
         shape = (D, group or D, "true" if group else "false")
         assert kernels(attention(fn, D=D, group=group)) == rows(*shape, 1)
-        assert kernels(attention(fn, T=4096, B=1, max_q=4096, W=64, D=D, group=group))[0] == tiles % shape
+        alone = ["k_kv4_attention_plan", tiles % shape, "k_kv4_attention_join_runs<%d, %d>" % shape[:2]]
+        assert kernels(attention(fn, T=4096, B=1, max_q=4096, W=64, D=D, group=group)) == alone
+        assert kernels(attention(fn, T=4000, B=8, max_q=500, W=64, D=D, group=group)) == alone + rows(*shape, 1)
         limit = {}
         for call in (attention(fn, D=D, group=group), attention(fn, T=320, max_q=5, D=D, group=group), attention(fn, T=4000, B=8, max_q=500, D=D, group=group)):
             for what, kernel, _, lds in launches([call])[0][2]:
@@ -58,15 +60,21 @@ def test_attention_takes_the_kernels_of_its_kind(fn):
 
 
 def test_rules_count_what_rows_may_see():
-    """Under a window the same table holds less to do: one block of rows, fewer parts, fewer workgroups, less scratch memory."""
+    """Under a window the same table holds less to do."""
     assert kernels(attention("window_attention", T=320, max_q=5, window=(1 << 31) - 1)) == rows(128, 128, "false", 2)
     assert kernels(attention("window_attention", T=320, max_q=5, window=300)) == rows(128, 128, "false", 1)
 
-    def grid(window):
-        (_, need, events), = launches([attention("window_attention", T=40, B=1, max_q=40, W=4000, Hkv=2, window=window)])
-        return need, [e[2] for e in events if e[0] == "launch"][0]
-    (all_need, everything), (need, some) = grid((1 << 31) - 1), grid(700)
-    assert some < everything / 8 and need < all_need / 4
+    def takes_tiles(**over):
+        return "k_kv4_attention_plan" in kernels(attention(**over))
+    for fn in ("window_attention", "tree_attention"):
+        assert takes_tiles(fn=fn, B=2, T=98, max_q=49, W=10)                        # more than 192 rows always do
+    much, little = dict(B=64, T=64 * 40, W=100), dict(B=4, T=160, W=60)
+    assert takes_tiles(fn="tree_attention", max_q=27, **much) and not takes_tiles(fn="tree_attention", max_q=26, **much)       # 108 and 104 rows
+    assert not takes_tiles(fn="tree_attention", max_q=48, **little)
+    assert not takes_tiles(fn="window_attention", max_q=40, window=100, **much)
+    # requests of few rows beside a prompt: a kernel of their own, unless they see little
+    many = dict(fn="window_attention", B=5, T=2004, max_q=2000, W=200)
+    assert len(kernels(attention(window=1000, **many))) == 3 and len(kernels(attention(window=4000, **many))) == 5
 
 
 def test_small_calls():
