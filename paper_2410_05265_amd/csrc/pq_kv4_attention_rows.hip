@@ -530,17 +530,15 @@ __global__ __launch_bounds__(kThreads, kPerCu) void k_kv4_attention_rows(Attenti
 #pragma unroll
                 for (int c = 0; c < CB; ++c) {
                     const int left = limit[c] - (t0 + 4 * quarter);
-                    if constexpr (MASKED) {
-                        uint32_t nodes = 0;        // of the tree, tokens that the query sees behind its limit
-                        if (tree && t0 + kTile > all_see)
-                            nodes = mask_bits(a, r, min(tile * ROWS + 16 * c + col, rows - 1) / per_kv, t0 - (r.sees - 1)) >> (4 * quarter);
-                        const int hidden = lo[c] - (t0 + 4 * quarter), front = a.sinks - (t0 + 4 * quarter);
+                    if constexpr (MASKED) {        // a bit for each of 32 tokens from this lane's first on
+                        auto below = [](int n) PQ_INLINE -> uint32_t { return n <= 0 ? 0 : n >= 32 ? ~0u : (1u << n) - 1; };
+                        uint32_t see = below(left) & (~below(lo[c] - (t0 + 4 * quarter)) | below(a.sinks - (t0 + 4 * quarter)));
+                        if (tree && t0 + kTile > all_see)          // nodes of its mask, behind the limit
+                            see |= (mask_bits(a, r, min(tile * ROWS + 16 * c + col, rows - 1) / per_kv, t0 - (r.sees - 1)) >> (4 * quarter)) & ~below(left);
+                        if (bad0) see &= 0xFFFF0000u;
+                        if (bad1) see &= 0x0000FFFFu;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int at = 16 * (j >> 2) + (j & 3);
-                            const bool sees_it = at < left ? at >= hidden || at < front : (nodes >> at) & 1;
-                            if (!sees_it || (j < 4 ? bad0 : bad1)) x[c][j] = -INFINITY;
-                        }
+                        for (int j = 0; j < 8; ++j) x[c][j] = (see >> (16 * (j >> 2) + (j & 3))) & 1 ? x[c][j] : -INFINITY;
                         continue;
                     }
 #pragma unroll
