@@ -626,8 +626,8 @@ int pq_kv4_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n
  * request and sees the prefix tokens and the cached tokens t <= p with
  *     t < sinks   or   t > p - window;
  * everything else is as in pq_kv4_attention with causal != 0.  window >= 1 (any number: one that is as long as the history hides nothing),
- * sinks >= 0.  Only pages with tokens that a row of the request sees are read, but for the ends of their 64 tokens: entries of the table in between may be
- * anything, -1 among it, as where a server has taken such pages back.
+ * sinks >= 0.  Entries of the table whose pages hold no token that a row of the request sees may be anything, -1 among it, as where a server has
+ * taken such pages back.
  * workspace: pq_kv4_window_attention_workspace_bytes of the same arguments (at most what pq_kv4_attention's says of itself). */
 size_t pq_kv4_window_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, int32_t window,
                                                int32_t sinks, const pq_kv4_cache* cache);
@@ -678,7 +678,7 @@ int pq_kv4_accept(const int32_t* tokens, const int32_t* parents, const int32_t* 
                   int32_t* kv_len_out, int64_t* from_slots, int64_t* to_slots, int32_t* taken_out, void* stream);
 
 /* pq_kv4_keep: the codes (and dynamic steps) of slot from_slots[b, k] go to slot to_slots[b, k], of every head, in every layer: caches, n_caches of
- * them on the host, of the same sizes.  Entries with a slot outside the cache move nothing.  In a row b, entry k may write where an earlier entry (or it
+ * them on the host, of the same sizes, no two with memory in common.  Entries with a slot outside the cache move nothing.  In a row b, entry k may write where an earlier entry (or it
  * itself) reads, as pq_kv4_accept's do; one that writes where a later one, or another row's, reads or writes leaves one or the other there.
  * 1 <= width <= 256;  B < 2^26, B * n_kv_heads < 2^30. */
 int pq_kv4_keep(const int64_t* from_slots, const int64_t* to_slots, int32_t B, int32_t width, const pq_kv4_cache* caches, int32_t n_caches,

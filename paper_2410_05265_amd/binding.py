@@ -1004,6 +1004,9 @@ class KV4Layers:
         first = self.tensors[0][0]
         if any(layer[0].shape != first.shape or layer[0].device != first.device for layer in self.tensors):
             raise ValueError("shape mismatch")
+        places = sorted((t.data_ptr(), t.numel() * t.element_size()) for layer in self.tensors for t in layer[:4 if self.group else 2])
+        if any(at + size > behind for (at, size), (behind, _) in zip(places, places[1:])):
+            raise ValueError("layers share memory")       # what one of them had moved, the other would move again
         self.device = first.get_device()
         self.caches = (KV4Cache * len(self.tensors))(*(_kv4_cache(*layer, self.group) for layer in self.tensors))
         self.count = len(self.tensors)

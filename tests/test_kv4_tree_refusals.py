@@ -219,7 +219,13 @@ def test_python_checks_shapes(b, monkeypatch):
     refused(b.KV4Layers, [])
     refused(b.KV4Layers, [codes, host_cache(pages=4)])
     refused(b.KV4Layers, [codes[:2] + (codes[2][:1], codes[3])])
-    layers = b.KV4Layers([codes, codes])
+    refused(b.KV4Layers, [codes, codes])                            # what one of them had moved, the other would move again
+    refused(b.KV4Layers, [(codes[0], codes[0]) + codes[2:]])
+    both, steps = torch.zeros((5, 2, 16, 32), dtype=torch.uint8), [torch.ones((3, 2, 16, 1)) for _ in range(4)]
+    refused(b.KV4Layers, [codes, (both[:3], both[2:]) + codes[2:]])
+    refused(b.KV4Layers, [codes[:2] + (steps[0], steps[1]), host_cache()[:2] + (steps[1], steps[2])], 64)
+    assert b.KV4Layers([codes[:2] + (steps[0], steps[1]), host_cache()[:2] + (steps[2], steps[3])], 64).count == 2
+    layers = b.KV4Layers([codes, host_cache()[:2] + codes[2:]])     # (static steps do not move)
     assert layers.count == 2 and layers.address == ctypes.addressof(layers.caches)
     slots = torch.zeros((2, 3), dtype=torch.int64)
     refused(b.pq_kv4_keep, slots, slots[:1], layers)
