@@ -193,7 +193,6 @@ template <int SIZE> struct Tiles {
 size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity);
 int launch_attention_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, float* partial, hipStream_t st);
 size_t masked_tiles_workspace_bytes(int64_t T, int32_t B, int32_t per_kv, int32_t head_dim, int small_rows);
-int launch_masked_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, void* ws, hipStream_t st);
 
 }  // namespace kv4
 }  // namespace pq

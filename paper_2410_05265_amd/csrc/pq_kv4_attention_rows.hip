@@ -14,7 +14,7 @@
 // A wavefront takes 32 tokens at a time.  Their codes go from memory straight into its ring of kDepth places in LDS, so three tiles are on
 // their way without a register; a lane then reads 16 bytes of a token's key codes (its part of every step of the first product), and 4
 // bytes of each of eight tokens' value codes: an 8 x 8 block, whose transposition is a byte permutation of two tokens.
-#include "pq_kv4_attention.h"
+#include "pq_kv4_attention_plan.h"
 
 #define PQ_INLINE __attribute__((always_inline))
 
@@ -778,15 +778,29 @@ __device__ __forceinline__ void join(const AttentionArgs& a, const float* __rest
 // Adds the partial sums of the histories that were cut: a workgroup takes four rows of one, one to a wavefront.
 constexpr int kJoinGroups = 1 << 16;     // (there may be more histories than a launch can have workgroups)
 template <int D, int CB>
-__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items)
+__device__ __forceinline__ void join_items(const AttentionArgs& a, const float* __restrict__ partial, const Item* __restrict__ items, uint32_t group, uint32_t groups)
 {
     const int lane = threadIdx.x & 63, row = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int count = items[0].parts;
-    Item item = items[1 + blockIdx.x];                                   // (of the last call, or nothing, from the count on)
-    for (int64_t i = blockIdx.x; i < count; i += gridDim.x) {
-        if (i != blockIdx.x) item = items[1 + i];
+    Item item = items[1 + group];                                        // (of the last call, or nothing, from the count on)
+    for (int64_t i = group; i < count; i += groups) {
+        if (i != group) item = items[1 + i];
         if (item.parts > 1 && item.row0 + row < item.rows) join<D, CB>(a, partial, item, row, lane);
     }
+}
+template <int D, int CB>
+__global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items)
+{
+    join_items<D, CB>(a, partial, items, blockIdx.x, gridDim.x);
+}
+
+// The same beside the plan of the tile kernel behind it, which one workgroup more makes meanwhile.
+template <int D, int CB>
+__global__ __launch_bounds__(kThreads) void k_kv4_attention_join_and_plan(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items, RunPlan p,
+                                                                          int runs, int small_rows)
+{
+    if (blockIdx.x > 0) join_items<D, CB>(a, partial, items, blockIdx.x - 1, gridDim.x - 1);
+    else if (blockIdx.y == 0) make_plan<kThreads>(a, p, runs, small_rows);
 }
 
 // What a call has at most: histories (of 16 rows), and workgroups with something to do.
@@ -807,7 +821,7 @@ size_t partial_bytes(int64_t groups, int32_t head_dim, int blocks)
 }
 
 template <int D, int G, bool DYNAMIC, int CB, typename... KIND>
-int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, hipStream_t st)
+int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, const TilePlan* tiles, hipStream_t st)
 {
     static std::atomic<uint64_t> allowed{0};
     constexpr size_t lds = Shape<D, G, DYNAMIC, CB>::kLds;
@@ -818,7 +832,14 @@ int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, h
     float* const partial = static_cast<float*>(ws);
     Item* const items = reinterpret_cast<Item*>(static_cast<uint8_t*>(ws) + partial_bytes(most.groups, D, CB));
     kernel<<<(unsigned)groups, kThreads, lds, st>>>(a, partial, items, most.items, small_rows);
-    k_kv4_attention_join<D, CB><<<dim3((unsigned)(most.items < kJoinGroups ? most.items : kJoinGroups), 4 * CB), kThreads, 0, st>>>(a, partial, items);
+    const unsigned joins = (unsigned)(most.items < kJoinGroups ? most.items : kJoinGroups);
+    if constexpr (sizeof...(KIND) > 0) {
+        if (tiles) {
+            k_kv4_attention_join_and_plan<D, CB><<<dim3(joins + 1, 4 * CB), kThreads, 0, st>>>(a, partial, items, tiles->plan, tiles->runs, small_rows);
+            return hip_status(hipGetLastError());
+        }
+    }
+    k_kv4_attention_join<D, CB><<<dim3(joins, 4 * CB), kThreads, 0, st>>>(a, partial, items);
     return hip_status(hipGetLastError());
 }
 
@@ -830,7 +851,7 @@ int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, h
 // registers twice (16 requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
 int blocks_for(int32_t max_q, int32_t per_kv, int64_t units) { return (int64_t)max_q * per_kv > 16 && units > 48 * kGroups * kWaves ? 2 : 1; }
 
-// The masked tile kernel cuts its work into equal runs and leaves out wavefronts without rows, so it is worth its three launches earlier, where a
+// The masked tile kernel cuts its work into equal runs and leaves out wavefronts without rows, so it is worth its launches earlier, where a
 // call has much to do.  Row | tile kernel, us, trees, 32 heads of 128 on 8, with 64, 104, 128 and 192 rows: 64 requests of up to 3000 tokens 94 | 115,
 // 128 | 126, 154 | 131, 205 | 159, with a step to 32 channels 161 | 253, 238 | 266, 293 | 283, 400 | 323; 16 of 4000 46 | 54, 66 | 62, 61 | 57,
 // 74 | 66; with less to do, 4 of 4000, 29 | 35, 30 | 38, 37 | 39, 43 | 47, one of 3000 23 | 33, 26 | 36, 27 | 36, 29 | 43.
@@ -860,17 +881,17 @@ size_t rows_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_
 }
 
 template <int CB, typename... KIND>
-int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, int64_t capacity, void* ws, hipStream_t st)
+int launch_rows(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, int64_t capacity, void* ws, const TilePlan* tiles, hipStream_t st)
 {
     if (head_dim == 64) {
-        if (group == 0) return launch<64, 64, false, CB, KIND...>(a, small_rows, capacity, ws, st);
-        if (group == 32) return launch<64, 32, true, CB, KIND...>(a, small_rows, capacity, ws, st);
-        return launch<64, 64, true, CB, KIND...>(a, small_rows, capacity, ws, st);
+        if (group == 0) return launch<64, 64, false, CB, KIND...>(a, small_rows, capacity, ws, tiles, st);
+        if (group == 32) return launch<64, 32, true, CB, KIND...>(a, small_rows, capacity, ws, tiles, st);
+        return launch<64, 64, true, CB, KIND...>(a, small_rows, capacity, ws, tiles, st);
     }
-    if (group == 0) return launch<128, 128, false, CB, KIND...>(a, small_rows, capacity, ws, st);
-    if (group == 32) return launch<128, 32, true, 1, KIND...>(a, small_rows, capacity, ws, st);
-    if (group == 64) return launch<128, 64, true, CB, KIND...>(a, small_rows, capacity, ws, st);
-    return launch<128, 128, true, CB, KIND...>(a, small_rows, capacity, ws, st);
+    if (group == 0) return launch<128, 128, false, CB, KIND...>(a, small_rows, capacity, ws, tiles, st);
+    if (group == 32) return launch<128, 32, true, 1, KIND...>(a, small_rows, capacity, ws, tiles, st);
+    if (group == 64) return launch<128, 64, true, CB, KIND...>(a, small_rows, capacity, ws, tiles, st);
+    return launch<128, 128, true, CB, KIND...>(a, small_rows, capacity, ws, tiles, st);
 }
 
 }  // namespace
@@ -889,16 +910,20 @@ int launch_attention(const AttentionArgs& a, int32_t head_dim, int32_t group, in
 {
     const Histories h = {(int64_t)a.table_pages << a.cache.log2_page, masked, a.window, a.sinks};
     const int small_rows = small_rows_for(max_q, a.heads_per_kv, a.B, a.cache.n_kv_heads, h);
-    if (small_rows != INT32_MAX) {
-        uint8_t* const partial = static_cast<uint8_t*>(ws) + rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, small_rows, h);
-        const int rc = masked ? launch_masked_tiles(a, head_dim, group, small_rows, partial, st)
-                              : launch_attention_tiles(a, head_dim, group, small_rows, reinterpret_cast<float*>(partial), st);
+    uint8_t* const tiles_ws = static_cast<uint8_t*>(ws) + rows_workspace_bytes(a.T, a.B, a.n_heads, a.cache.n_kv_heads, head_dim, max_q, small_rows, h);
+    const bool some_tiles = small_rows != INT32_MAX;
+    if (some_tiles && !masked) {
+        const int rc = launch_attention_tiles(a, head_dim, group, small_rows, reinterpret_cast<float*>(tiles_ws), st);
         if (rc != PQ_OK || small_rows == 0) return rc;
     }
+    const TilePlan plan = some_tiles && masked ? plan_of(a, head_dim, group, small_rows, tiles_ws) : TilePlan{};
+    if (masked && small_rows == 0) return launch_masked_tiles(a, head_dim, group, small_rows, plan, false, st);
     const int64_t capacity = h.seen_by(max_q), units = at_most(a.T, a.B, a.n_heads, a.cache.n_kv_heads, capacity, small_rows).units;
     const bool one = blocks_for(max_q, a.heads_per_kv, units) == 1;
-    if (masked) return one ? launch_rows<1, Masked>(a, head_dim, group, small_rows, capacity, ws, st) : launch_rows<2, Masked>(a, head_dim, group, small_rows, capacity, ws, st);
-    return one ? launch_rows<1>(a, head_dim, group, small_rows, capacity, ws, st) : launch_rows<2>(a, head_dim, group, small_rows, capacity, ws, st);
+    auto rows = [&](auto launch) { return launch(a, head_dim, group, small_rows, capacity, ws, some_tiles ? &plan : nullptr, st); };
+    if (!masked) return one ? rows(launch_rows<1>) : rows(launch_rows<2>);
+    const int rc = one ? rows(launch_rows<1, Masked>) : rows(launch_rows<2, Masked>);
+    return rc != PQ_OK || !some_tiles ? rc : launch_masked_tiles(a, head_dim, group, small_rows, plan, true, st);
 }
 
 }  // namespace kv4

@@ -11,7 +11,7 @@
 // a workgroup's start and end take as long as five of its steps, of which it has 26 on average, and 5 % of the products meet the mask.
 //
 // Where a call has few tiles of rows, the histories are cut into `splits` parts; their sums go through scratch memory and a second kernel.
-#include "pq_kv4_attention.h"
+#include "pq_kv4_attention_plan.h"
 
 #define PQ_INLINE __attribute__((always_inline))
 
@@ -24,6 +24,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 512, kWaves = 8;
 constexpr int kRows = kTileRows, kCols = 32;      // rows of a workgroup and of a wavefront
 constexpr int kTile = 64;                         // tokens of a step
+static_assert(kTile == kPlanStep, "units");
 constexpr int kPrefixTile = 32;
 constexpr int kJoinThreads = 256;
 constexpr float kLeast = 0x1.0p-80f;
@@ -38,8 +39,7 @@ struct Where {
 
 __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r, int small_rows)
 {
-    const int64_t rows = (int64_t)r.q_len * a.heads_per_kv;
-    return rows <= small_rows ? 0 : (int)((rows + kRows - 1) / kRows);
+    return row_tiles_of(a, r, small_rows);
 }
 
 // For many requests: `starts`, tiles before each request and in all.  A workgroup that walks over the requests itself reads all of them, and
@@ -120,46 +120,8 @@ __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index
     return {lanes(b), lanes(tile), {lanes(r.start), lanes(r.q_len), lanes(r.n), lanes(r.sees)}};
 }
 
-// ---- The masked variant's work is cut into runs.  What a tile of rows sees differs more there (windows, trees beside prompts), and so do the
-// requests: all steps of the call, request after request, in each head after head and tile of rows after tile, lie one after another, and every
-// workgroup takes an equal run of them, whatever the lengths are (a chiplet's workgroups read neighbouring rows' tokens of one head: with the
-// heads inside the tiles the codes missed its L2, prompts took 1.4 times as long).  A tile and head that a run covers whole is written as it is; of one that is cut, the workgroups leave
-// partial sums (at most two each), and a second kernel adds them.  The tiles and where the runs begin are listed by a kernel of one workgroup in
-// front: planned by every workgroup for itself they cost 40 us of code that is run once and has to come from memory.
-
-// A run is counted in units: a tile and head has one for every step and kTileUnits in front, for what it takes beside its steps (queries, prefix,
-// results; without them a run of many short tiles took up to 1.3 times as long as one of few long ones).
-constexpr int kTileUnits = 5;
-
-// A tile of rows: `steps` of 64 tokens (0: it sees nothing), of which those from Tiles::front on lie `gap` further.
-struct RowTile {
-    int b, tile, of, steps, gap;         // of: tiles of the request
-    Request r;
-};
-__device__ __forceinline__ int units_of(int steps) { return kTileUnits + max(steps, 1); }
-// Of a workgroup, its first unit: of a tile and head; tile < 0: it has none.
-struct Start {
-    int tile, head, unit, unused;
-    int64_t length, each;        // units of the run, and of one that is not the last
-};
-// A tile that was cut, by the workgroup that began it: `parts` workgroups from it on have some of it (0: none was).
-struct Cut {
-    int parts, start, rows, head, row0, unused[3];
-};
 // Runs: a workgroup to a CU, two where registers let two run there.
 template <int D, bool DYNAMIC> constexpr int kRuns = D == 64 && !DYNAMIC ? 512 : 256;
-constexpr int kMostRuns = 512, kFewestUnits = 7;
-
-// Scratch memory of the masked variant.
-struct Plan {
-    Start* starts;               // [kMostRuns]
-    Cut* cuts;                   // [kMostRuns]
-    RowTile* tiles;              // [most_tiles]
-    int64_t* units_before;       // [most_tiles + 1], of one head
-    int32_t* tiles_before;       // [B + 1], of each request
-    float* partial;              // two places for each run
-    int most_tiles;
-};
 
 // What the kernels are given beside the call's arguments: scratch memory, and how it is used.
 template <typename... KIND> struct Work {
@@ -168,7 +130,7 @@ template <typename... KIND> struct Work {
     int splits, small_rows;
 };
 template <> struct Work<Masked> {
-    Plan plan;
+    RunPlan plan;
 };
 struct PlainParts { float* partial; const int32_t* starts; int splits, small_rows; };
 struct MaskedParts { float* partial; const Start* starts; int splits, small_rows; };
@@ -189,97 +151,10 @@ template <typename T> __device__ __forceinline__ T for_all(const T* from)
     return v;
 }
 
-constexpr int kPlanThreads = 1024;
-// Inclusive sum over the workgroup; `all`: the sum.
-__device__ __forceinline__ int64_t sum_up(int64_t v, int64_t* sums, int tid, int64_t& all)
+constexpr int kPlanThreads = 1024;       // (alone; beside the row kernel's second one it has that one's)
+__global__ __launch_bounds__(kPlanThreads) void k_kv4_attention_plan(AttentionArgs a, RunPlan p, int runs, int small_rows)
 {
-    const int lane = tid & 63, wave = tid >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t x = __shfl_up(v, d, 64);
-        if (lane >= d) v += x;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = v;
-    __syncthreads();
-    all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        if (w < wave) v += sums[w];
-        all += sums[w];
-    }
-    return v;
-}
-// The last place whose entry is at most x.
-template <typename T> __device__ __forceinline__ int place_in(const T* list, int n, int64_t x)
-{
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (list[mid] <= x) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
-
-__global__ __launch_bounds__(kPlanThreads) void k_kv4_attention_plan(AttentionArgs a, Plan p, int runs, int small_rows)
-{
-    __shared__ int64_t sums[kPlanThreads / 64], few_units[kPlanThreads + 1];
-    __shared__ int32_t few_tiles[kPlanThreads + 1];
-    const int tid = threadIdx.x, Hkv = a.cache.n_kv_heads, per_kv = a.heads_per_kv;
-    int32_t* const tiles_before = a.B <= kPlanThreads ? few_tiles : p.tiles_before;
-    const int each = (a.B + kPlanThreads - 1) / kPlanThreads, first = min(tid * each, a.B), last = min(first + each, a.B);
-    int64_t own = 0, all;
-    for (int b = first; b < last; ++b) own += tiles_of(a, request(a, b), small_rows);
-    int64_t at = sum_up(own, sums, tid, all) - own;
-    for (int b = first; b < last; ++b) {
-        tiles_before[b] = (int32_t)min(at, (int64_t)INT32_MAX);
-        if (last - first > 1) at += tiles_of(a, request(a, b), small_rows);
-    }
-    // (only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
-    const int tiles = (int)min(all, (int64_t)p.most_tiles);
-    int64_t* const units_before = tiles <= kPlanThreads ? few_units : p.units_before;
-    __syncthreads();
-    int64_t total = 0;
-    for (int t0 = 0; t0 < tiles; t0 += kPlanThreads) {
-        const int t = t0 + tid;
-        int64_t units = 0, sum;
-        if (t < tiles) {
-            // (the last of the requests that begin there: those in front of it have no tiles)
-            const int b = place_in(tiles_before, a.B, t);
-            const Request r = request(a, b);
-            const int tile = t - tiles_before[b], row0 = tile * kRows;
-            const Seen seen = masked_rows(a, r, row0 / per_kv, min((row0 + kRows - 1) / per_kv, r.q_len - 1));
-            const Tiles<kTile> left(a, seen.lo);
-            const int count = left.count(seen.any);
-            p.tiles[t] = {b, tile, tiles_of(a, r, small_rows), count, left.gap, r};
-            units = units_of(count);
-        }
-        const int64_t incl = sum_up(units, sums, tid, sum);
-        if (t < tiles) units_before[t] = total + incl - units;
-        total += sum;
-    }
-    if (tid == 0) units_before[tiles] = total;
-    __syncthreads();
-    const int64_t units = total * Hkv, length = max((units + runs - 1) / runs, (int64_t)kFewestUnits);
-    if (tid >= runs) return;
-    p.cuts[tid].parts = 0;
-    const int64_t begin = length * tid;
-    Start s = {-1, 0, 0, 0, min(length, units - begin), length};
-    if (begin < units) {
-        int lo = 0, hi = a.B - 1;                  // the request
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (units_before[min(tiles_before[mid], tiles)] * Hkv <= begin) lo = mid;
-            else hi = mid - 1;
-        }
-        const int first_tile = tiles_before[lo], end_tile = lo + 1 < a.B ? min(tiles_before[lo + 1], tiles) : tiles;
-        const int64_t base = units_before[first_tile], one = units_before[end_tile] - base, in = begin - base * Hkv;
-        s.head = (int)(in / one);
-        const int64_t at_unit = base + in - s.head * one;
-        s.tile = first_tile + place_in(units_before + first_tile, end_tile - first_tile, at_unit);
-        s.unit = (int)(at_unit - units_before[s.tile]);
-    }
-    p.starts[tid] = s;
+    make_plan<kPlanThreads>(a, p, runs, small_rows);
 }
 
 // Row `at` of the accumulators as a channel: channels of a group lie so in LDS that neighbouring threads of the expansion write
@@ -950,7 +825,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_tiles(Atten
 // The same for the tiles that runs have cut: a workgroup takes 64 rows and 64 channels of one, a thread 16 channels of a row.  The loads of four
 // parts are on their way at once (one after another, and 32 channels to a thread: 10 tiles of rows x 8 heads in four parts each 32 us).
 template <int D, int G>
-__global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_runs(AttentionArgs a, Plan p)
+__global__ __launch_bounds__(kJoinThreads) void k_kv4_attention_join_runs(AttentionArgs a, RunPlan p)
 {
     constexpr int kAtOnce = 4, kChannels = 16;
     const Cut cut = p.cuts[blockIdx.x];
@@ -1054,10 +929,9 @@ int launch_plain(const AttentionArgs& a, int64_t groups, const Work<>& work, hip
 }
 
 template <int D, int G, bool DYNAMIC>
-int launch_masked(const AttentionArgs& a, int small_rows, const Work<Masked>& work, hipStream_t st)
+int launch_masked(const AttentionArgs& a, const Work<Masked>& work, hipStream_t st)
 {
     constexpr int runs = kRuns<D, DYNAMIC>;
-    k_kv4_attention_plan<<<1, kPlanThreads, 0, st>>>(a, work.plan, runs, small_rows);
     if (const int rc = launch<D, G, DYNAMIC, Masked>(a, runs, work, st); rc != PQ_OK) return rc;
     k_kv4_attention_join_runs<D, G><<<dim3(runs, kRows / 64, D / 64), kJoinThreads, 0, st>>>(a, work.plan);
     return hip_status(hipGetLastError());
@@ -1079,7 +953,7 @@ int64_t masked_tiles_at_most(int64_t T, int32_t B, int32_t per_kv, int small_row
 
 size_t up_to_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // The masked variant's scratch memory, at `ws`; its size.
-size_t lay_out(Plan* p, void* ws, int64_t most_tiles, int32_t B, int32_t head_dim)
+size_t lay_out(RunPlan* p, void* ws, int64_t most_tiles, int32_t B, int32_t head_dim)
 {
     uint8_t* const base = static_cast<uint8_t*>(ws);
     size_t at = 0;
@@ -1091,8 +965,8 @@ size_t lay_out(Plan* p, void* ws, int64_t most_tiles, int32_t B, int32_t head_di
     p->starts = reinterpret_cast<Start*>(take(kMostRuns * sizeof(Start)));
     p->cuts = reinterpret_cast<Cut*>(take(kMostRuns * sizeof(Cut)));
     p->tiles = reinterpret_cast<RowTile*>(take((size_t)most_tiles * sizeof(RowTile)));
-    p->units_before = reinterpret_cast<int64_t*>(take(most_tiles > kPlanThreads ? (size_t)(most_tiles + 1) * sizeof(int64_t) : 0));
-    p->tiles_before = reinterpret_cast<int32_t*>(take(B > kPlanThreads ? (size_t)(B + 1) * sizeof(int32_t) : 0));
+    p->units_before = reinterpret_cast<int64_t*>(take(most_tiles > kFewestPlanThreads ? (size_t)(most_tiles + 1) * sizeof(int64_t) : 0));
+    p->tiles_before = reinterpret_cast<int32_t*>(take(B > kFewestPlanThreads ? (size_t)(B + 1) * sizeof(int32_t) : 0));
     p->partial = reinterpret_cast<float*>(take((size_t)(head_dim == 64 ? kMostRuns : 256) * 2 * kRows * (head_dim + 2) * sizeof(float)));
     p->most_tiles = (int)most_tiles;
     return at;
@@ -1102,23 +976,34 @@ size_t lay_out(Plan* p, void* ws, int64_t most_tiles, int32_t B, int32_t head_di
 
 size_t masked_tiles_workspace_bytes(int64_t T, int32_t B, int32_t per_kv, int32_t head_dim, int small_rows)
 {
-    Plan p;
+    RunPlan p;
     return lay_out(&p, nullptr, masked_tiles_at_most(T, B, per_kv, small_rows), B, head_dim);
 }
 
-int launch_masked_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, void* ws, hipStream_t st)
+TilePlan plan_of(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, void* ws)
 {
-    Work<Masked> w;
-    lay_out(&w.plan, ws, masked_tiles_at_most(a.T, a.B, a.heads_per_kv, small_rows), a.B, head_dim);
-    if (head_dim == 64) {
-        if (group == 0) return launch_masked<64, 64, false>(a, small_rows, w, st);
-        if (group == 32) return launch_masked<64, 32, true>(a, small_rows, w, st);
-        return launch_masked<64, 64, true>(a, small_rows, w, st);
+    TilePlan t;
+    lay_out(&t.plan, ws, masked_tiles_at_most(a.T, a.B, a.heads_per_kv, small_rows), a.B, head_dim);
+    t.runs = head_dim == 128 ? kRuns<128, false> : group == 0 ? kRuns<64, false> : kRuns<64, true>;
+    return t;
+}
+
+int launch_masked_tiles(const AttentionArgs& a, int32_t head_dim, int32_t group, int small_rows, const TilePlan& plan, bool made, hipStream_t st)
+{
+    if (!made) {
+        k_kv4_attention_plan<<<1, kPlanThreads, 0, st>>>(a, plan.plan, plan.runs, small_rows);
+        if (const int rc = hip_status(hipGetLastError()); rc != PQ_OK) return rc;
     }
-    if (group == 0) return launch_masked<128, 128, false>(a, small_rows, w, st);
-    if (group == 32) return launch_masked<128, 32, true>(a, small_rows, w, st);
-    if (group == 64) return launch_masked<128, 64, true>(a, small_rows, w, st);
-    return launch_masked<128, 128, true>(a, small_rows, w, st);
+    const Work<Masked> w = {plan.plan};
+    if (head_dim == 64) {
+        if (group == 0) return launch_masked<64, 64, false>(a, w, st);
+        if (group == 32) return launch_masked<64, 32, true>(a, w, st);
+        return launch_masked<64, 64, true>(a, w, st);
+    }
+    if (group == 0) return launch_masked<128, 128, false>(a, w, st);
+    if (group == 32) return launch_masked<128, 32, true>(a, w, st);
+    if (group == 64) return launch_masked<128, 64, true>(a, w, st);
+    return launch_masked<128, 128, true>(a, w, st);
 }
 
 size_t tiles_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int64_t capacity)
