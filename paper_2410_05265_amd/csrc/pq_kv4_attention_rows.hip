@@ -754,20 +754,27 @@ __device__ __forceinline__ void add_parts(Joined<D>& j, const float* __restrict_
     j.top = to;
 }
 
+// Parts n0 .. end - 1 of a row.
 template <int D, int CB>
-__device__ __forceinline__ void join(const AttentionArgs& a, const float* __restrict__ partial, const Item& item, int row, int lane)
+__device__ __forceinline__ Joined<D> add_up(const float* __restrict__ partial, const Item& item, int row, int n0, int end, int lane)
 {
-    constexpr int ROWS = 16 * CB, kEach = D / 64;
+    constexpr int ROWS = 16 * CB;
     Joined<D> j;
     const float* const first = partial + ((int64_t)item.worker * 2 * ROWS + row) * (D + 4);
     const int64_t step = 2 * ROWS * (D + 4), second = item.second ? ROWS * (D + 4) : 0;
-    int n0 = 0;
-    for (; item.parts - n0 > 8; n0 += 64) {
-        const int n = min(item.parts - n0, 64);
+    for (; end - n0 > 8; n0 += 64) {
+        const int n = min(end - n0, 64);
         if (n > 32) add_parts<D, 64>(j, first, step, second, n0, n, lane);
         else add_parts<D, 32>(j, first, step, second, n0, n, lane);
     }
-    if (n0 < item.parts) add_parts<D, 8>(j, first, step, second, n0, item.parts - n0, lane);
+    if (n0 < end) add_parts<D, 8>(j, first, step, second, n0, end - n0, lane);
+    return j;
+}
+
+template <int D>
+__device__ __forceinline__ void write_joined(const AttentionArgs& a, const Joined<D>& j, const Item& item, int row, int lane)
+{
+    constexpr int kEach = D / 64;
     const float f = j.sum > 0.0f ? 1.0f / j.sum : 0.0f;
     const int at_row = item.row0 + row, per_kv = a.heads_per_kv;
     __half* dst = a.out + ((int64_t)(item.start + at_row / per_kv) * a.n_heads + item.head * per_kv + at_row % per_kv) * D + kEach * lane;
@@ -785,7 +792,7 @@ __device__ __forceinline__ void join_items(const AttentionArgs& a, const float* 
     Item item = items[1 + group];                                        // (of the last call, or nothing, from the count on)
     for (int64_t i = group; i < count; i += groups) {
         if (i != group) item = items[1 + i];
-        if (item.parts > 1 && item.row0 + row < item.rows) join<D, CB>(a, partial, item, row, lane);
+        if (item.parts > 1 && item.row0 + row < item.rows) write_joined<D>(a, add_up<D, CB>(partial, item, row, 0, item.parts, lane), item, row, lane);
     }
 }
 template <int D, int CB>
@@ -794,13 +801,56 @@ __global__ __launch_bounds__(kThreads) void k_kv4_attention_join(AttentionArgs a
     join_items<D, CB>(a, partial, items, blockIdx.x, gridDim.x);
 }
 
-// The same beside the plan of the tile kernel behind it, which one workgroup more makes meanwhile.
+// The same with a workgroup to a row, each of its wavefronts adding a quarter of the parts.
 template <int D, int CB>
-__global__ __launch_bounds__(kThreads) void k_kv4_attention_join_and_plan(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items, RunPlan p,
-                                                                          int runs, int small_rows)
+__device__ __forceinline__ void join_items_together(const AttentionArgs& a, const float* __restrict__ partial, const Item* __restrict__ items, uint32_t group, uint32_t groups)
 {
-    if (blockIdx.x > 0) join_items<D, CB>(a, partial, items, blockIdx.x - 1, gridDim.x - 1);
-    else if (blockIdx.y == 0) make_plan<kThreads>(a, p, runs, small_rows);
+    constexpr int kEach = D / 64;
+    __shared__ float quarters[kWaves][2 + kEach][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.y;
+    const int count = items[0].parts;
+    for (int64_t i = group; i < count; i += groups) {
+        const Item item = items[1 + i];
+        if (item.parts <= 1 || item.row0 + row >= item.rows) continue;
+        const int each = (item.parts + kWaves - 1) / kWaves, from = min(wave * each, item.parts);
+        Joined<D> j = add_up<D, CB>(partial, item, row, from, min(from + each, item.parts), lane);
+        quarters[wave][0][lane] = j.top;
+        quarters[wave][1][lane] = j.sum;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) quarters[wave][2 + k][lane] = j.acc[k];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) {
+                const float top = quarters[w][0][lane], to = fmaxf(j.top, top), old = __builtin_amdgcn_exp2f(j.top - to), f = __builtin_amdgcn_exp2f(top - to);
+                j.top = to;
+                j.sum = fmaf(j.sum, old, quarters[w][1][lane] * f);
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) j.acc[k] = fmaf(j.acc[k], old, quarters[w][2 + k][lane] * f);
+            }
+            write_joined<D>(a, j, item, row, lane);
+        }
+        __syncthreads();                           // (read before the next item's)
+    }
+}
+
+// Behind the masked row kernel; where the tile kernel comes then (runs > 0), one workgroup more makes its plan meanwhile.  Few histories, of many parts
+// each, are joined by workgroups together.  A wavefront | a workgroup to a row, us of the whole call, 32 heads of 128 on 8: one token over 1600
+// tokens (8 histories) 13.5 | 12.1, over 12000 33.1 | 20.9, over 50000 36.4 | 27.7; 8 nodes over 12000 (24) 28.2 | 24.0; four requests' tokens over
+// 12000 (40) 25.0 | 22.4; 26 nodes over 3000 (56) 25.4 | 26.0; four requests of 26 over 4000 (over 200) 29.9 | 32.9.
+constexpr int kFewItems = 48;
+template <int D, int CB, bool TOGETHER>
+__global__ __launch_bounds__(kThreads) void k_kv4_attention_join_masked(AttentionArgs a, const float* __restrict__ partial, const Item* __restrict__ items, RunPlan p,
+                                                                        int runs, int small_rows)
+{
+    const uint32_t plans = runs > 0 ? 1 : 0;
+    if (blockIdx.x < plans) {
+        if (blockIdx.y == 0) make_plan<kThreads>(a, p, runs, small_rows);
+    } else if constexpr (TOGETHER) {
+        join_items_together<D, CB>(a, partial, items, blockIdx.x - plans, gridDim.x - plans);
+    } else {
+        join_items<D, CB>(a, partial, items, blockIdx.x - plans, gridDim.x - plans);
+    }
 }
 
 // What a call has at most: histories (of 16 rows), and workgroups with something to do.
@@ -834,12 +884,13 @@ int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, c
     kernel<<<(unsigned)groups, kThreads, lds, st>>>(a, partial, items, most.items, small_rows);
     const unsigned joins = (unsigned)(most.items < kJoinGroups ? most.items : kJoinGroups);
     if constexpr (sizeof...(KIND) > 0) {
-        if (tiles) {
-            k_kv4_attention_join_and_plan<D, CB><<<dim3(joins + 1, 4 * CB), kThreads, 0, st>>>(a, partial, items, tiles->plan, tiles->runs, small_rows);
-            return hip_status(hipGetLastError());
-        }
+        const TilePlan then = tiles ? *tiles : TilePlan{};
+        const unsigned groups = joins + (tiles ? 1 : 0);
+        if (most.items <= kFewItems) k_kv4_attention_join_masked<D, CB, true><<<dim3(groups, 16 * CB), kThreads, 0, st>>>(a, partial, items, then.plan, then.runs, small_rows);
+        else k_kv4_attention_join_masked<D, CB, false><<<dim3(groups, 4 * CB), kThreads, 0, st>>>(a, partial, items, then.plan, then.runs, small_rows);
+    } else {
+        k_kv4_attention_join<D, CB><<<dim3(joins, 4 * CB), kThreads, 0, st>>>(a, partial, items);
     }
-    k_kv4_attention_join<D, CB><<<dim3(joins, 4 * CB), kThreads, 0, st>>>(a, partial, items);
     return hip_status(hipGetLastError());
 }
 

@@ -37,8 +37,8 @@ def attention(fn, **over):
     return c
 
 
-def rows(D, G, dynamic, blocks):
-    return ["k_kv4_attention_rows<%d, %d, %s, %d, pq::kv4::Masked>" % (D, G, dynamic, blocks), "k_kv4_attention_join<%d, %d>" % (D, blocks)]
+def rows(D, G, dynamic, blocks, together="false"):
+    return ["k_kv4_attention_rows<%d, %d, %s, %d, pq::kv4::Masked>" % (D, G, dynamic, blocks), "k_kv4_attention_join_masked<%d, %d, %s>" % (D, blocks, together)]
 
 
 @pytest.mark.parametrize("fn", ["window_attention", "tree_attention"])
@@ -49,7 +49,7 @@ def test_attention_takes_the_kernels_of_its_kind(fn):
         assert kernels(attention(fn, D=D, group=group)) == rows(*shape, 1)
         many = [tiles % shape, "k_kv4_attention_join_runs<%d, %d>" % shape[:2]]
         assert kernels(attention(fn, T=4096, B=1, max_q=4096, W=64, D=D, group=group)) == ["k_kv4_attention_plan"] + many
-        assert kernels(attention(fn, T=4000, B=8, max_q=500, W=64, D=D, group=group)) == [rows(*shape, 1)[0], "k_kv4_attention_join_and_plan<%d, 1>" % D] + many
+        assert kernels(attention(fn, T=4000, B=8, max_q=500, W=64, D=D, group=group)) == rows(*shape, 1) + many
         limit = {}
         for call in (attention(fn, D=D, group=group), attention(fn, T=320, max_q=5, D=D, group=group), attention(fn, T=4000, B=8, max_q=500, D=D, group=group)):
             for what, kernel, _, lds in launches([call])[0][2]:
@@ -77,6 +77,11 @@ def test_rules_count_what_rows_may_see():
     assert len(kernels(attention(window=1000, **many))) == 3 and len(kernels(attention(window=4000, **many))) == 4
 
 
+def test_few_histories_are_joined_by_workgroups():
+    for B, T, max_q, together in ((1, 1, 1, "true"), (1, 8, 8, "true"), (4, 4, 1, "true"), (1, 26, 26, "false"), (16, 16, 1, "false")):
+        assert kernels(attention("tree_attention", B=B, T=T, max_q=max_q)) == rows(128, 128, "false", 1, together)
+
+
 def test_small_calls():
     for B, T in ((1, 26), (300, 5000), ((1 << 26) - 1, 5), (7, (1 << 30) - 1)):
         (rc, _, events), = launches([dict(fn="tree", B=B, T=T, words=8)])
@@ -102,7 +107,8 @@ def test_largest_sizes_stay_within_a_launch():
             assert need <= (160 << 20) + 2 * (call["T"] * call["Hq"] + 16 * call["B"] * call["Hkv"])
             for what, kernel, grid, _ in events:
                 threads = 512 if "_tiles<" in kernel and "join" not in kernel else 256
-                y = 4 if "join_tiles" in kernel else 8 if ("_join<" in kernel or "_join_and_plan<" in kernel) and kernel.endswith("2>") else 4 if "join" in kernel else 1
+                masked = "join_masked" in kernel
+                y = (16 if "true" in kernel else 4) * (2 if ", 2," in kernel else 1) if masked else 4 if "join" in kernel else 1
                 assert what == "allow" or 0 < grid // y * threads < 1 << 32, (call, kernel, grid)
 
 
