@@ -28,7 +28,7 @@ constexpr int kTileUnits = 5;
 
 // A tile of rows: `steps` of 64 tokens (0: it sees nothing), of which those from Tiles::front on lie `gap` further.
 struct RowTile {
-    int b, tile, of, steps, gap;         // of: tiles of the request
+    int b, tile, of, steps, gap;         // of: tiles of the request, as far as they are listed
     Request r;
 };
 __device__ __forceinline__ int units_of(int steps) { return kTileUnits + max(steps, 1); }
@@ -42,6 +42,28 @@ struct Cut {
     int parts, start, rows, head, row0, unused[3];
 };
 constexpr int kMostRuns = 512, kFewestUnits = 7;
+
+// A run goes on to the tile and head behind `t`, of whose units it has taken `take`: the request's next tile, or its first one of the next head.
+__device__ __forceinline__ void walk_on(Start& run, const RowTile& t, int take, int n_kv_heads)
+{
+    run.length -= take;
+    run.unit = 0;
+    ++run.tile;
+    if (t.tile + 1 == t.of && run.head + 1 < n_kv_heads) {
+        ++run.head;
+        run.tile -= t.of;
+    } else if (t.tile + 1 == t.of) {
+        run.head = 0;
+    }
+}
+
+// Tiles of requests of more than small_rows rows, at most: 256 rows of one at least, or the rows of a smaller one.
+inline int64_t masked_tiles_at_most(int64_t T, int32_t B, int32_t per_kv, int small_rows)
+{
+    const int64_t rows = T * per_kv, by_requests = rows / kTileRows + B, fewest = small_rows + 1 < (kTileRows + 1) / 2 ? small_rows + 1 : (kTileRows + 1) / 2;
+    const int64_t by_rows = rows / fewest + 1;
+    return by_requests < by_rows ? by_requests : by_rows;
+}
 
 // Scratch memory of the masked variant.
 struct RunPlan {
@@ -109,7 +131,7 @@ template <int THREADS> __device__ __forceinline__ void make_plan(const Attention
         tiles_before[b] = (int32_t)min(at, (int64_t)INT32_MAX);
         if (last - first > 1) at += row_tiles_of(a, request(a, b), small_rows);
     }
-    // (only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places)
+    // (only rows that lie in two requests, from a cu_q that does not ascend, make more than there are places: then the last ones are in no list)
     const int tiles = (int)min(all, (int64_t)p.most_tiles);
     int64_t* const units_before = tiles <= THREADS ? few_units : p.units_before;
     __syncthreads();
@@ -125,7 +147,7 @@ template <int THREADS> __device__ __forceinline__ void make_plan(const Attention
             const Seen seen = masked_rows(a, r, row0 / per_kv, min((row0 + kTileRows - 1) / per_kv, r.q_len - 1));
             const Tiles<kPlanStep> left(a, seen.lo);
             const int count = left.count(seen.any);
-            p.tiles[t] = {b, tile, row_tiles_of(a, r, small_rows), count, left.gap, r};
+            p.tiles[t] = {b, tile, min(row_tiles_of(a, r, small_rows), tiles - tiles_before[b]), count, left.gap, r};
             units = units_of(count);
         }
         const int64_t incl = sum_up<THREADS>(units, sums, tid, sum);

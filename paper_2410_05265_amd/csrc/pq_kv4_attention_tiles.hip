@@ -267,15 +267,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && !DYNAMIC ? 4 : 2) void k_kv4_a
             for (int64_t left = units - last; left > 0; left -= run.each) ++parts;
             cuts[worker] = {parts, at.r.start, at.r.q_len * per_kv, head, at.tile * kRows, {0, 0, 0}};
         }
-        run.length -= take;
-        run.unit = 0;
-        ++run.tile;
-        if (row_tile.tile + 1 == row_tile.of && run.head + 1 < Hkv) {
-            ++run.head;
-            run.tile -= row_tile.of;
-        } else if (row_tile.tile + 1 == row_tile.of) {
-            run.head = 0;
-        }
+        walk_on(run, row_tile, take, Hkv);
         held.run = run;
         more_units = (int)min(run.length, (int64_t)kTileUnits + 1);
         next_index = run.tile;
@@ -941,14 +933,6 @@ int launch_masked(const AttentionArgs& a, const Work<Masked>& work, hipStream_t 
 size_t tiles_partial_bytes(int64_t tiles, int splits, int32_t n_kv_heads, int32_t head_dim)
 {
     return splits > 1 ? (size_t)(tiles * n_kv_heads * splits) * kRows * (head_dim + 2) * sizeof(float) : 0;
-}
-
-// Of the masked variant, with requests of more than small_rows rows: 256 rows of one at least, or the rows of a smaller one.
-int64_t masked_tiles_at_most(int64_t T, int32_t B, int32_t per_kv, int small_rows)
-{
-    const int64_t rows = T * per_kv, by_requests = rows / kRows + B, fewest = small_rows + 1 < (kRows + 1) / 2 ? small_rows + 1 : (kRows + 1) / 2;
-    const int64_t by_rows = rows / fewest + 1;
-    return by_requests < by_rows ? by_requests : by_rows;
 }
 
 size_t up_to_256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
