@@ -702,6 +702,32 @@ def pq_calibrate_static_zp(x_cal, had_block: int, n_gamma: int = 8, n_beta: int 
     return res
 
 
+_MOST = (1 << 31) - 1
+_WHOLE = {name: tuple(i for i, t in enumerate(args) if t is _i32) for name, (_, args) in SIGNATURES.items() if name.startswith("pq_kv4")}
+
+
+def _fits(name: str, args) -> bool:
+    """Whether the numbers of a call are the library's 32 bits: ctypes would cut them off, and take 2^32 + 16 for 16."""
+    return all(-_MOST - 1 <= args[i] <= _MOST for i in _WHOLE[name])
+
+
+def _run(name: str, *args):
+    fn = getattr(lib(), name)
+    if not _fits(name, args):
+        raise PQError(PQ_ERR_SHAPE, name)
+    _check(fn(*args), name)
+
+
+def _bytes(name: str, *args) -> int:
+    """A workspace's size; 0 for sizes that the call refuses."""
+    return int(getattr(lib(), name)(*args)) if _fits(name, args) else 0
+
+
+def _any(v) -> int:
+    """A number that may be of any size: one past 32 bits says the same as the largest."""
+    return min(int(v), _MOST)
+
+
 def pq_kv4_slots(kv_len, q_len, block_table, free_pages, page_size: int, T: int, taken=None, position_offset: int = 0, cu_q=None,
                  kv_len_out=None, positions=None, slots=None, taken_out=None):
     """Places for a step's new tokens: kv_len, q_len int32 [B], block_table int32 [B, pages] (new entries are written), free_pages int32,
@@ -737,10 +763,16 @@ def pq_kv4_slots(kv_len, q_len, block_table, free_pages, page_size: int, T: int,
     if (q_len.numel() != B or block_table.dim() != 2 or block_table.shape[0] != B or cu_q.numel() < B + 1 or kv_len_out.numel() < B or
             positions.numel() < T or slots.numel() < T or taken_out.numel() < 1 or (taken is not None and taken.numel() < 1)):
         raise ValueError("shape mismatch")
-    _check(lib().pq_kv4_slots(_ptr(kv_len), _ptr(q_len), B, _ptr(block_table), block_table.shape[1], _ptr(free_pages), free_pages.numel(),
-                              _ptr(taken), int(page_size), int(T), int(position_offset), _ptr(cu_q), _ptr(kv_len_out), _ptr(positions),
-                              _ptr(slots), _ptr(taken_out), _stream()), "pq_kv4_slots")
+    _run("pq_kv4_slots", _ptr(kv_len), _ptr(q_len), B, _ptr(block_table), block_table.shape[1], _ptr(free_pages), free_pages.numel(), _ptr(taken),
+         int(page_size), int(T), int(position_offset), _ptr(cu_q), _ptr(kv_len_out), _ptr(positions), _ptr(slots), _ptr(taken_out), _stream())
     return cu_q, kv_len_out, positions, slots, taken_out
+
+
+def _cache_of(places, shape, group: int):
+    n_pages, heads, page_size, half = shape
+    if max(heads, page_size, 2 * half, abs(group)) > _MOST:        # (the structure's fields would be cut off as well)
+        raise ValueError("sizes past 32 bits")
+    return KV4Cache(*places, n_pages, heads, 2 * half, page_size, group)
 
 
 def _kv4_cache(k_codes, v_codes, k_scale, v_scale, group: int):
@@ -755,7 +787,7 @@ def _kv4_cache(k_codes, v_codes, k_scale, v_scale, group: int):
     steps = heads if group <= 0 else n_pages * heads * page_size * (2 * half // group)
     if k_scale.numel() != steps or v_scale.numel() != steps:
         raise ValueError("shape mismatch")
-    return KV4Cache(_ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale), n_pages, heads, 2 * half, page_size, int(group))
+    return _cache_of((_ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale)), k_codes.shape, int(group))
 
 
 def _rows(t: torch.Tensor, what: str):
@@ -802,16 +834,15 @@ def pq_kv4_append(qkv, n_heads: int, positions, slots, k_codes, v_codes, k_scale
     else:
         _here(out, torch.float16, "out")
         _result(out, T * n_heads * D, "out")
-    _check(lib().pq_kv4_append(_ptr(qkv), qkv.stride(0) if T > 1 else qkv.shape[1], T, int(n_heads), _ptr(positions), _ptr(slots), _ptr(q_weight),
-                               _ptr(k_weight), float(eps), _ptr(cos_sin), 0 if cos_sin is None else cos_sin.shape[0], rd, int(bool(interleaved)),
-                               int(bool(rotate)), float(clip), cache, _ptr(out), _stream()), "pq_kv4_append")
+    _run("pq_kv4_append", _ptr(qkv), qkv.stride(0) if T > 1 else qkv.shape[1], T, int(n_heads), _ptr(positions), _ptr(slots), _ptr(q_weight),
+         _ptr(k_weight), float(eps), _ptr(cos_sin), 0 if cos_sin is None else cos_sin.shape[0], rd, int(bool(interleaved)), int(bool(rotate)),
+         float(clip), cache, _ptr(out), _stream())
     return out
 
 
 def _kv4_sizes(k_codes):
     """A cache's sizes, for a workspace query."""
-    n_pages, heads, page_size, half = k_codes.shape
-    return KV4Cache(None, None, None, None, n_pages, heads, 2 * half, page_size, 0)
+    return _cache_of((None, None, None, None), k_codes.shape, 0)
 
 
 def _kv4_attend(name, q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v, sight, sizes, out, workspace):
@@ -834,7 +865,7 @@ def _kv4_attend(name, q, cu_q, kv_len, block_table, cache, softmax_scale, max_q,
                 raise ValueError("shape mismatch")
     W = block_table.shape[1]
     if workspace is None:
-        need = int(getattr(lib(), name + "_workspace_bytes")(T, B, n_heads, int(max_q), W, *sizes, cache))
+        need = _bytes(name + "_workspace_bytes", T, B, n_heads, _any(max_q), W, *sizes, cache)
         workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=q.device)
     else:
         _here(workspace, torch.uint8, "workspace")
@@ -843,15 +874,14 @@ def _kv4_attend(name, q, cu_q, kv_len, block_table, cache, softmax_scale, max_q,
     else:
         _here(out, torch.float16, "out")
         _result(out, T * n_heads * D, "out")
-    _check(getattr(lib(), name)(_ptr(q), q.stride(0) if T > 1 else q.shape[1], T, n_heads, _ptr(cu_q), _ptr(kv_len), B, int(max_q),
-                                _ptr(block_table), W, cache, _ptr(prefix_k), _ptr(prefix_v), n_prefix, float(softmax_scale), *sight,
-                                _ptr(out), _ptr(workspace), workspace.numel(), _stream()), name)
+    _run(name, _ptr(q), q.stride(0) if T > 1 else q.shape[1], T, n_heads, _ptr(cu_q), _ptr(kv_len), B, _any(max_q), _ptr(block_table), W, cache,
+         _ptr(prefix_k), _ptr(prefix_v), n_prefix, float(softmax_scale), *sight, _ptr(out), _ptr(workspace), workspace.numel(), _stream())
     return out, workspace
 
 
 def pq_kv4_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, k_codes) -> int:
     """Scratch memory of pq_kv4_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
-    return int(lib().pq_kv4_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), _kv4_sizes(k_codes)))
+    return _bytes("pq_kv4_attention_workspace_bytes", T, B, int(n_heads), _any(max_q), int(table_pages), _kv4_sizes(k_codes))
 
 
 def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, group: int = 0,
@@ -874,8 +904,7 @@ def pq_kv4_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_
 
 def pq_kv4_window_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, window: int, sinks: int, k_codes) -> int:
     """Scratch memory of pq_kv4_window_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
-    return int(lib().pq_kv4_window_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), int(window), int(sinks),
-                                                             _kv4_sizes(k_codes)))
+    return _bytes("pq_kv4_window_attention_workspace_bytes", T, B, int(n_heads), _any(max_q), int(table_pages), _any(window), _any(sinks), _kv4_sizes(k_codes))
 
 
 def pq_kv4_window_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, window: int,
@@ -891,7 +920,7 @@ def pq_kv4_window_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_sc
         if rc > 0:
             raise PQError(rc, "pq_kv4_window_attention")
     cache = _kv4_cache(k_codes, v_codes, k_scale, v_scale, group)
-    sight = (int(window), int(sinks))
+    sight = (_any(window), _any(sinks))
     return _kv4_attend("pq_kv4_window_attention", q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v, sight, sight,
                        out, workspace)
 
@@ -908,6 +937,8 @@ def pq_kv4_tree(parents, cu_q, kv_len, words: int, position_offset: int = 0, mas
         if rc > 0:
             raise PQError(rc, "pq_kv4_tree")
     T, B = parents.numel(), kv_len.numel()
+    if not 1 <= int(words) <= 8:                                   # (in front of an allocation by it)
+        raise PQError(PQ_ERR_SHAPE, "pq_kv4_tree")
     if mask is None:
         mask = torch.empty((T, int(words)), dtype=torch.int32, device=parents.device)
     if positions is None:
@@ -916,15 +947,13 @@ def pq_kv4_tree(parents, cu_q, kv_len, words: int, position_offset: int = 0, mas
         _here(t, torch.int32, what)
     if cu_q.numel() != B + 1 or mask.numel() < T * int(words) or positions.numel() < T:
         raise ValueError("shape mismatch")
-    _check(lib().pq_kv4_tree(_ptr(parents), _ptr(cu_q), _ptr(kv_len), B, T, int(words), int(position_offset), _ptr(mask), _ptr(positions),
-                             _stream()), "pq_kv4_tree")
+    _run("pq_kv4_tree", _ptr(parents), _ptr(cu_q), _ptr(kv_len), B, T, int(words), int(position_offset), _ptr(mask), _ptr(positions), _stream())
     return mask, positions
 
 
 def pq_kv4_tree_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: int, table_pages: int, window: int, sinks: int, k_codes) -> int:
     """Scratch memory of pq_kv4_tree_attention; sizes of the cache from k_codes uint8 [pages, kv heads, page_size, head_dim / 2]."""
-    return int(lib().pq_kv4_tree_attention_workspace_bytes(T, B, int(n_heads), int(max_q), int(table_pages), int(window), int(sinks),
-                                                           _kv4_sizes(k_codes)))
+    return _bytes("pq_kv4_tree_attention_workspace_bytes", T, B, int(n_heads), _any(max_q), int(table_pages), _any(window), _any(sinks), _kv4_sizes(k_codes))
 
 
 def pq_kv4_tree_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, mask,
@@ -944,7 +973,7 @@ def pq_kv4_tree_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scal
     _here(mask, torch.int32, "mask")
     if mask.dim() != 2 or mask.shape[0] != q.shape[0]:
         raise ValueError("shape mismatch")
-    size = (int(window), int(sinks))
+    size = (_any(window), _any(sinks))
     return _kv4_attend("pq_kv4_tree_attention", q, cu_q, kv_len, block_table, cache, softmax_scale, max_q, prefix_k, prefix_v,
                        (_ptr(mask), mask.shape[1]) + size, size, out, workspace)
 
@@ -964,7 +993,7 @@ def pq_kv4_accept(tokens, parents, chosen, cu_q, kv_len, block_table, page_size:
         if rc > 0:
             raise PQError(rc, "pq_kv4_accept")
     T, B, depth = tokens.numel(), kv_len.numel(), int(depth)
-    if depth < 1:
+    if not 1 <= depth <= 256:
         raise PQError(PQ_ERR_SHAPE, "pq_kv4_accept")
     sizes = (("accepted", B), ("next_token", B), ("path", B * depth), ("kv_len_out", B), ("from_slots", B * depth), ("to_slots", B * depth), ("taken_out", 1))
     made = []
@@ -986,9 +1015,9 @@ def pq_kv4_accept(tokens, parents, chosen, cu_q, kv_len, block_table, page_size:
     if (parents.numel() != T or chosen.numel() != T or cu_q.numel() != B + 1 or block_table.dim() != 2 or block_table.shape[0] != B or
             (taken is not None and taken.numel() < 1)):
         raise ValueError("shape mismatch")
-    _check(lib().pq_kv4_accept(_ptr(tokens), _ptr(parents), _ptr(chosen), _ptr(cu_q), _ptr(kv_len), B, T, int(words), depth, _ptr(block_table),
-                               block_table.shape[1], int(page_size), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), _ptr(taken),
-                               *(_ptr(t) for t in made), _stream()), "pq_kv4_accept")
+    _run("pq_kv4_accept", _ptr(tokens), _ptr(parents), _ptr(chosen), _ptr(cu_q), _ptr(kv_len), B, T, int(words), depth, _ptr(block_table),
+         block_table.shape[1], int(page_size), _ptr(free_pages), 0 if free_pages is None else free_pages.numel(), _ptr(taken),
+         *(_ptr(t) for t in made), _stream())
     return tuple(made)
 
 
@@ -1028,8 +1057,7 @@ def pq_kv4_keep(from_slots, to_slots, layers: KV4Layers):
         raise ValueError("shape mismatch")
     if layers.device != torch._C._cuda_getDevice():
         raise ValueError("layers must lie on the current device")
-    _check(lib().pq_kv4_keep(_ptr(from_slots), _ptr(to_slots), from_slots.shape[0], from_slots.shape[1], layers.caches, layers.count, _stream()),
-           "pq_kv4_keep")
+    _run("pq_kv4_keep", _ptr(from_slots), _ptr(to_slots), from_slots.shape[0], from_slots.shape[1], layers.caches, layers.count, _stream())
 
 
 def pq_set_gemm_variant(variant: int) -> int:
