@@ -628,7 +628,8 @@ int pq_kv4_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n
  * everything else is as in pq_kv4_attention with causal != 0.  window >= 1 (any number: one that is as long as the history hides nothing),
  * sinks >= 0.  Entries of the table whose pages hold no token that a row of the request sees may be anything, -1 among it, as where a server has
  * taken such pages back.
- * workspace: pq_kv4_window_attention_workspace_bytes of the same arguments (at most what pq_kv4_attention's says of itself). */
+ * workspace: pq_kv4_window_attention_workspace_bytes of the same arguments (at most what pq_kv4_attention's says of itself and 96 bytes for each
+ * request). */
 size_t pq_kv4_window_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, int32_t window,
                                                int32_t sinks, const pq_kv4_cache* cache);
 int pq_kv4_window_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* cu_q, const int32_t* kv_len,
