@@ -17,6 +17,7 @@ constexpr int kMostWidth = 256;
 // 256 of them with 4 steps each 46 -> 11; 16 requests with 32 heads in 32 layers 17.2 -> 10.8.  48 requests with 6 entries in 80 layers:
 // 16.1 us for 368 640 pieces of 64 bytes and their steps, read and written, nearly each in a line of its own.
 constexpr int kWavefronts = 4096;
+constexpr int kMostHeads = 1 << 16;      // of a wavefront: what it has to move is counted in 32 bits, 256 entries of up to four pieces each
 
 struct Layers {
     struct {
@@ -83,8 +84,9 @@ void launch(const Layers& layers, int n, const int64_t* from_slots, const int64_
 {
     const int groups = B < 1 << 16 ? B : 1 << 16;
     const int64_t parts = kWavefronts / ((int64_t)groups * n);
-    const int heads = parts < 2 ? c.n_kv_heads : parts >= c.n_kv_heads ? 1 : (int)((c.n_kv_heads + parts - 1) / parts);
-    k_kv4_keep<D, NG><<<dim3((unsigned)groups, (unsigned)n, (unsigned)((c.n_kv_heads + heads - 1) / heads)), 64, 0, st>>>(
+    const int shared = parts < 2 ? c.n_kv_heads : parts >= c.n_kv_heads ? 1 : (int)((c.n_kv_heads + parts - 1) / parts);
+    const int heads = shared < kMostHeads ? shared : kMostHeads;
+    k_kv4_keep<D, NG><<<dim3((unsigned)groups, (unsigned)n, (unsigned)(((int64_t)c.n_kv_heads + heads - 1) / heads)), 64, 0, st>>>(
         layers, from_slots, to_slots, B, width, c.n_pages * c.page_size, c.n_kv_heads, heads, __builtin_ctz((unsigned)c.page_size));
 }
 
