@@ -653,7 +653,11 @@ int pq_kv4_tree(const int32_t* parents, const int32_t* cu_q, const int32_t* kv_l
  * and the tokens t < c with
  *     t < sinks   or   t >= c + (nodes that it sees) - window;
  * rows of prompts see what pq_kv4_window_attention says.  window = 0: no window.  A row that sees nothing gets zeros.  Everything else, the
- * workspace's size with it, is as in pq_kv4_window_attention. */
+ * workspace's size with it, is as in pq_kv4_window_attention.
+ * The window hides history alone.  What a row sees of the tree is its mask's business: with pq_kv4_tree's masks a node sees its whole branch, also
+ * nodes that stand `window` or more above it, which the same token decoded by itself, or in a prompt, would not see.  Where branches may be deeper
+ * than the window, clear the bits of those nodes: of row t the nodes j with positions[j] <= positions[t] - window, but for first tokens
+ * (positions[j] - position_offset < sinks).  Each row then sees what pq_kv4_window_attention shows a token at its position. */
 size_t pq_kv4_tree_attention_workspace_bytes(int64_t T, int32_t B, int32_t n_heads, int32_t max_q, int32_t table_pages, int32_t window,
                                              int32_t sinks, const pq_kv4_cache* cache);
 int pq_kv4_tree_attention(const void* q_f16, int64_t row_stride, int64_t T, int32_t n_heads, const int32_t* cu_q, const int32_t* kv_len,

@@ -959,7 +959,8 @@ def pq_kv4_tree_attention_workspace_bytes(T: int, B: int, n_heads: int, max_q: i
 def pq_kv4_tree_attention(q, cu_q, kv_len, block_table, k_codes, v_codes, k_scale, v_scale, softmax_scale: float, max_q: int, mask,
                           window: int = 0, sinks: int = 0, group: int = 0, prefix_k=None, prefix_v=None, out=None, workspace=None):
     """pq_kv4_attention, where the last tokens of a request of up to 32 * words rows are the nodes of a tree and a row sees those of its mask
-    (int32 [T, words], pq_kv4_tree's); window 0: all of the history.  Returns (out, workspace)."""
+    (int32 [T, words], pq_kv4_tree's); window 0: all of the history.  The window hides history alone: where branches are deeper than it, clear the
+    mask's bits of nodes that stand `window` or more above the row's own.  Returns (out, workspace)."""
     if out is not None and workspace is not None:
         if _lib is None:
             lib()
