@@ -142,12 +142,14 @@ __device__ __forceinline__ const RowTile* tiles_of(const Work<>&) { return nullp
 __device__ __forceinline__ const RowTile* tiles_of(const Work<Masked>& w) { return w.plan.tiles; }
 
 // What lies there, as scalars: where a branch goes by it, and barriers stand behind the branch, the wavefronts go whole.
+// (Words of 64-bit members and pointers: as `int` the compiler might take them for other memory than the members that were written.)
+typedef int word_of_any __attribute__((may_alias));
 template <typename T> __device__ __forceinline__ T for_all(const T* from)
 {
     T v;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(T) / 4); ++i)
-        reinterpret_cast<int*>(&v)[i] = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(from)[i]);
+        reinterpret_cast<word_of_any*>(&v)[i] = __builtin_amdgcn_readfirstlane(reinterpret_cast<const word_of_any*>(from)[i]);
     return v;
 }
 
