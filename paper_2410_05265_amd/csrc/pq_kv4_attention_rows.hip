@@ -902,13 +902,17 @@ int launch(const AttentionArgs& a, int small_rows, int64_t capacity, void* ws, c
 // the work are faster.  One | two, us, 32 heads of 128 on 8: 16 requests of 2000 to 4000 tokens with 20 rows 36 | 34, 32 rows (32000 units) 37 |
 // 40, 64 rows 50 | 48, 128 rows (128000) 78 | 66; 64 requests with 20 rows (up to 128000) 81 | 66, 32 rows 84 | 78, 128 rows 261 | 197; one of
 // 131072 with 48 rows (98000) 85 | 75; one step to a head, 64 requests, 128 rows 297 | 229.  Four groups of dynamic steps would not fit the
-// registers twice (16 requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).
+// registers twice (16 requests, 64 rows 64 | 85; 64 requests, 128 rows 326 | 339).  The masked kernel's two blocks with a step to 64 channels spill 8
+// registers and are worth it: 64 trees of up to 3000 tokens, one | two blocks, 96, 104, 128 and 160 rows 232 | 180, 256 | 218, 318 | 241, 362 | 271.
 int blocks_for(int32_t max_q, int32_t per_kv, int64_t units) { return (int64_t)max_q * per_kv > 16 && units > 48 * kGroups * kWaves ? 2 : 1; }
 
 // The masked tile kernel cuts its work into equal runs and leaves out wavefronts without rows, so it is worth its launches earlier, where a
 // call has much to do.  Row | tile kernel, us, trees, 32 heads of 128 on 8, with 64, 104, 128 and 192 rows: 64 requests of up to 3000 tokens 94 | 115,
 // 128 | 126, 154 | 131, 205 | 159, with a step to 32 channels 161 | 253, 238 | 266, 293 | 283, 400 | 323; 16 of 4000 46 | 54, 66 | 62, 61 | 57,
-// 74 | 66; with less to do, 4 of 4000, 29 | 35, 30 | 38, 37 | 39, 43 | 47, one of 3000 23 | 33, 26 | 36, 27 | 36, 29 | 43.
+// 74 | 66; with less to do, 4 of 4000, 29 | 35, 30 | 38, 37 | 39, 43 | 47, one of 3000 23 | 33, 26 | 36, 27 | 36, 29 | 43.  Just above the border, with
+// 108, 112, 120 and 160 rows, 64 requests of up to 3000: static steps 172 | 135, 166 | 129, 178 | 137, 200 | 164; one step to 128 channels 190 | 177,
+// 193 | 182, 198 | 185, 239 | 224; to 64 222 | 212, 220 | 208, 231 | 219, 271 | 262; to 32 311 | 279, 351 | 312, 370 | 298, 439 | 340.  16 of 4000:
+// 67 | 59, 69 | 61, 67 | 59, 82 | 75; 78 | 78, 78 | 81, 75 | 78, 89 | 92; 89 | 90, 92 | 96, 90 | 92, 97 | 103; 115 | 114, 121 | 120, 134 | 122, 131 | 115.
 constexpr int kMaskedSmallRows = 104;
 constexpr int64_t kMuch = 4096;          // steps of 64 tokens, of all requests and heads
 int border_for(int32_t B, int32_t n_kv_heads, int32_t per_kv, const Histories& h)
@@ -918,7 +922,11 @@ int border_for(int32_t B, int32_t n_kv_heads, int32_t per_kv, const Histories& h
 bool takes_tiles(int32_t max_q, int32_t per_kv, int border) { return (int64_t)max_q * per_kv > border; }
 // A single request is the tile kernel's whatever its rows are: the two launches that would find nothing to do take 4 us (1024 tokens of one
 // prompt, 32 heads on 8: 38 us with them, 34 without); with the masked one, which spreads a single row's steps over all workgroups as well, also some
-// that see little, four steps to a workgroup at most.
+// that see little, four steps to a workgroup at most.  Two row launches more | all rows in tiles, us, one prompt and B - 1 tokens, 32 heads of 128 on 8,
+// by the tokens' steps in all: 54 steps (B 2, window 256) prompts of 300, 1500 and 3100 47 | 42, 54 | 46, 75 | 69; 590 (B 5, 1000) 49 | 41, 75 | 67,
+// 108 | 103; 872 (B 17, 256) 49 | 41, 57 | 56, 81 | 63; 1090 (B 5, 2000) 54 | 48, 97 | 96, 155 | 151; 2180 (B 9, 2000) 56 | 56, 101 | 87, 158 | 161; 4360
+// (B 17, 2000) 61 | 71, 107 | 120, 164 | 180.  (A prompt of 2000 tokens is 256 tiles and heads, one to a run and none cut, and any more cut them: 46 | 54.)
+// Trees of 26 gain longer, their rows fill more of a tile: beside 300 tokens 750 steps 66 | 51, 4125 98 | 74, 11625 153 | 131.
 int small_rows_for(int32_t max_q, int32_t per_kv, int32_t B, int32_t n_kv_heads, const Histories& h)
 {
     const int border = border_for(B, n_kv_heads, per_kv, h);

@@ -120,7 +120,10 @@ __device__ __forceinline__ Where find_tile(const AttentionArgs& a, int64_t index
     return {lanes(b), lanes(tile), {lanes(r.start), lanes(r.q_len), lanes(r.n), lanes(r.sees)}};
 }
 
-// Runs: a workgroup to a CU, two where registers let two run there.
+// Runs: a workgroup to a CU, two where registers let two run there (64 channels, static steps; 9 registers are spilled then).  One | two, us, 32 heads on
+// 8: 2 prompts of up to 6000, window 1024 182 | 170, 4 of 4000, window 512 179 | 163, 8 chunks of 500 behind 3500, window 1024 80 | 72, one of 12000,
+// window 4096 503 | 462; 32 trees of 64 over up to 6000 130 | 125, 64 of 40 over up to 3000 136 | 121, 16 of 64 over 20000 261 | 243.  Where there is
+// little for them all, two lose: one prompt of 600, window 256 32 | 39, one tree of 64 over 8000 with 64 heads 44 | 52.
 template <int D, bool DYNAMIC> constexpr int kRuns = D == 64 && !DYNAMIC ? 512 : 256;
 
 // What the kernels are given beside the call's arguments: scratch memory, and how it is used.
